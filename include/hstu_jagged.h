@@ -195,6 +195,50 @@ size_t hstu_jagged_attn_workspace_bytes(int32_t B, int32_t max_len, int32_t H,
                                         const hstu_rab *rab);
 
 /* ---------------------------------------------------------------------------
+ * The same attention with a sliding window and a few first tokens that stay
+ * visible (sinks), for long histories:
+ *
+ *   a_ij = silu(s_ij) / N   for j <= i and (i - j < window or j < sinks), else 0
+ *
+ * -- a token sees itself and the window - 1 tokens before it, and the sequence's
+ * first `sinks` tokens.  Scores, biases, LayerNorm, layouts, types and errors are
+ * those of the plain calls, and so are `out` and `io`; window >= max_len or
+ * sinks >= max_len is the plain operator.  window = 0 leaves the sinks alone, and
+ * rows that then see nothing have o = 0, y = 0 and zero gradients.  The pairs that
+ * are not seen leave no trace: a NaN or an infinity in a row of q, k, v or dy
+ * reaches only rows that see it or are seen by it (and the table entries of such
+ * pairs).
+ *
+ * Work and memory grow with total_tokens x (window + sinks).  The backward of
+ * HSTU_BF16 takes a further workspace for the sinks' gradients over the queries
+ * past their windows, at most a quarter of q's size and 2 x 64 x d x H floats per
+ * sequence and 64 sinks.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int32_t window;              /* >= 0                                     */
+    int32_t sinks;               /* >= 0                                     */
+} hstu_window;
+
+size_t hstu_jagged_window_attn_workspace_bytes(int32_t B, int32_t max_len,
+                                               int32_t H, int32_t d,
+                                               int64_t total_tokens,
+                                               int32_t for_bwd, hstu_dtype dtype,
+                                               const hstu_rab *rab,
+                                               const hstu_window *win);
+
+int hstu_jagged_window_attn_fwd(const void *q, const void *k, const void *v,
+                                const void *u, const int64_t *seq_offsets,
+                                int32_t B, int32_t max_len, int32_t H, int32_t d,
+                                const hstu_rab *rab, const hstu_window *win,
+                                hstu_fwd_out *out, void *stream);
+
+int hstu_jagged_window_attn_bwd(const void *q, const void *k, const void *v,
+                                const void *u, const int64_t *seq_offsets,
+                                int32_t B, int32_t max_len, int32_t H, int32_t d,
+                                const hstu_rab *rab, const hstu_window *win,
+                                hstu_bwd_io *io, void *stream);
+
+/* ---------------------------------------------------------------------------
  * HSTU layer shell.  The attention above is the middle of one HSTU layer of
  * the models the paper trains (HSTU / FuXi, Appendix A "Parameter Settings").
  * These calls run a whole layer around it, with the library's reading of the

@@ -17,10 +17,11 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libhstu_jagged.so")
 ARCH = "gfx950"
-SOURCES = ["api.cpp", "sched.hip", "attn_bf16.hip", "attn_short.hip", "attn_f32.hip", "norm.hip",
-           "layer.cpp", "layer_kernels.hip", "noalloc.hip", "embedding.hip", "rab.hip",
-           "gemm.hip"]
-HEADERS = ["device.h", "internal.h", "sched_impl.h", "attn_common.h"]
+SOURCES = ["api.cpp", "sched.hip", "attn_bf16.hip", "attn_window.hip", "attn_short.hip",
+           "attn_f32.hip", "attn_window_f32.hip", "norm.hip", "layer.cpp", "layer_kernels.hip",
+           "noalloc.hip", "embedding.hip", "rab.hip", "gemm.hip"]
+HEADERS = ["device.h", "internal.h", "sched_impl.h", "attn_common.h", "attn_bf16_impl.h",
+           "attn_f32_impl.h"]
 
 CFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -34,7 +35,8 @@ CFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # returned value waits for the atomic at once (and with it for every load
 # and atomic in flight), instead of where the value is first used, a step
 # later.
-FILE_FLAGS = {"attn_bf16.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]}
+_POP = ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]
+FILE_FLAGS = {"attn_bf16.hip": _POP, "attn_window.hip": _POP}
 
 # The layer shell's GEMMs run on hipBLASLt.
 LDFLAGS = ["-L/opt/rocm/lib", "-lhipblaslt"]

@@ -88,6 +88,16 @@ int validate(const void *q, const void *k, const void *v, const void *u,
   return HSTU_OK;
 }
 
+int set_window(const hstu_window *win, Problem *p) {
+  if (!win) return HSTU_OK;
+  if (win->window < 0) return fail(HSTU_EINVAL, "window = %d < 0", win->window);
+  if (win->sinks < 0) return fail(HSTU_EINVAL, "sinks = %d < 0", win->sinks);
+  p->windowed = true;
+  p->window = std::min(win->window, p->N);
+  p->sinks = std::min(win->sinks, p->N);
+  return HSTU_OK;
+}
+
 int check_workspace_bytes(size_t need, void *ws, size_t bytes) {
   if (!ws) return fail(HSTU_EWORKSPACE, "workspace is NULL (%zu bytes needed)", need);
   if ((uintptr_t)ws % kAlign)
@@ -215,6 +225,20 @@ Layout make_layout(const Problem &p, bool for_bwd, int dev) {
                  : bf16_bwd ? take(sizeof(int64_t) * (size_t)DTIME_BINS * p.H * p.nb)
                  : f32_bwd  ? take(sizeof(int64_t) * (size_t)p.H * p.nb)
                             : 0;
+  // windowed backward with sinks: the query tiles past far_after see only sinks of
+  // the first key tile
+  if (bf16_bwd && p.windowed && p.sinks > 0) {
+    const int64_t tiles = ceil_div(p.N, TILE), reach = ((int64_t)TILE - 2 + p.window) / TILE;
+    const int64_t sink_tiles = ceil_div(p.sinks, TILE);
+    if (reach < tiles - 1) {
+      L.far_after = (int32_t)reach;
+      L.far_chunk = (int32_t)(FAR_CHUNK * sink_tiles);
+      L.far_entries = p.T / ((int64_t)TILE * L.far_chunk) + p.B;
+      L.list_f = take(sizeof(WorkEntry) * (size_t)std::max<int64_t>(L.far_entries, 1));
+      L.far_part = take(sizeof(float) * 2 * TILE * (size_t)p.d * p.H * (size_t)sink_tiles *
+                        (size_t)std::max<int64_t>(L.far_entries, 1));
+    }
+  }
   L.total = at;
   return L;
 }
@@ -222,13 +246,14 @@ Layout make_layout(const Problem &p, bool for_bwd, int dev) {
 
 int attn_fwd_call(const void *q, const void *k, const void *v, const void *u,
                   const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
-                  int32_t d, const hstu_rab *rab, hstu_fwd_out *out, void *stream,
-                  const FixedScratch *fixed) {
+                  int32_t d, const hstu_rab *rab, const hstu_window *win, hstu_fwd_out *out,
+                  void *stream, const FixedScratch *fixed) {
   clear_last_error();
   if (!out) return fail(HSTU_EINVAL, "out is NULL");
   Problem p;
   int rc = validate(q, k, v, u, seq_offsets, B, max_len, H, d, rab, out->dtype,
                     out->total_tokens, &p);
+  if (rc == HSTU_OK) rc = set_window(win, &p);
   if (rc != HSTU_OK) return rc;
   if (p.T > 0 && (!out->y || !out->o || !out->ln_mean || !out->ln_rstd))
     return fail(HSTU_EINVAL, "out->y, o, ln_mean and ln_rstd must be non-null");
@@ -281,12 +306,13 @@ int attn_fwd_call(const void *q, const void *k, const void *v, const void *u,
 
 int attn_bwd_call(const void *q, const void *k, const void *v, const void *u,
                   const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
-                  int32_t d, const hstu_rab *rab, hstu_bwd_io *io, void *stream,
-                  const GradOut *go) {
+                  int32_t d, const hstu_rab *rab, const hstu_window *win, hstu_bwd_io *io,
+                  void *stream, const GradOut *go) {
   if (!io) return fail(HSTU_EINVAL, "io is NULL");
   Problem p;
   int rc = validate(q, k, v, u, seq_offsets, B, max_len, H, d, rab, io->dtype,
                     io->total_tokens, &p);
+  if (rc == HSTU_OK) rc = set_window(win, &p);
   if (rc != HSTU_OK) return rc;
   if (go && p.dtype != HSTU_BF16)
     return fail(HSTU_ENOTSUP, "fused gradient outputs need HSTU_BF16");
@@ -413,7 +439,8 @@ int hstu_jagged_attn_fwd(const void *q, const void *k, const void *v,
                          const void *u, const int64_t *seq_offsets, int32_t B,
                          int32_t max_len, int32_t H, int32_t d,
                          const hstu_rab *rab, hstu_fwd_out *out, void *stream) {
-  return attn_fwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, out, stream, nullptr);
+  return attn_fwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, nullptr, out, stream,
+                       nullptr);
 }
 
 int hstu_jagged_attn_bwd(const void *q, const void *k, const void *v,
@@ -421,7 +448,46 @@ int hstu_jagged_attn_bwd(const void *q, const void *k, const void *v,
                          int32_t max_len, int32_t H, int32_t d,
                          const hstu_rab *rab, hstu_bwd_io *io, void *stream) {
   g_last_error.clear();
-  return attn_bwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, io, stream, nullptr);
+  return attn_bwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, nullptr, io, stream,
+                       nullptr);
+}
+
+size_t hstu_jagged_window_attn_workspace_bytes(int32_t B, int32_t max_len, int32_t H, int32_t d,
+                                               int64_t total_tokens, int32_t for_bwd,
+                                               hstu_dtype dtype, const hstu_rab *rab,
+                                               const hstu_window *win) {
+  g_last_error.clear();
+  if (!win) {
+    fail(HSTU_EINVAL, "win is NULL");
+    return 0;
+  }
+  Problem p;
+  static const char dummy = 0;
+  if (validate(&dummy, &dummy, &dummy, &dummy, (const int64_t *)&dummy, B, max_len, H, d, rab,
+               dtype, total_tokens, &p) != HSTU_OK ||
+      set_window(win, &p) != HSTU_OK)
+    return 0;
+  int dev = 0;
+  if (current_device(&dev) != HSTU_OK) return 0;
+  return make_layout(p, for_bwd != 0, dev).total;
+}
+
+int hstu_jagged_window_attn_fwd(const void *q, const void *k, const void *v, const void *u,
+                                const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
+                                int32_t d, const hstu_rab *rab, const hstu_window *win,
+                                hstu_fwd_out *out, void *stream) {
+  g_last_error.clear();
+  if (!win) return fail(HSTU_EINVAL, "win is NULL");
+  return attn_fwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, win, out, stream, nullptr);
+}
+
+int hstu_jagged_window_attn_bwd(const void *q, const void *k, const void *v, const void *u,
+                                const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
+                                int32_t d, const hstu_rab *rab, const hstu_window *win,
+                                hstu_bwd_io *io, void *stream) {
+  g_last_error.clear();
+  if (!win) return fail(HSTU_EINVAL, "win is NULL");
+  return attn_bwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, win, io, stream, nullptr);
 }
 
 int hstu_jagged_status(const void *workspace, int32_t *status, void *stream) {

@@ -770,11 +770,11 @@ auto pick_bwd(bool pos, bool time) {
 static int64_t short_items(const Problem &p) { return 2 * p.max_entries * p.H; }
 
 bool fwd_short(const Problem &p, int dev) {
-  return p.dtype == HSTU_BF16 &&
+  return p.dtype == HSTU_BF16 && !p.windowed &&
          short_items(p) <= (p.d == 64 ? 3 : 1) * (int64_t)device_info(dev).num_cu;
 }
 bool bwd_short(const Problem &p, int dev) {
-  return p.dtype == HSTU_BF16 &&
+  return p.dtype == HSTU_BF16 && !p.windowed &&
          2 * short_items(p) <= (p.d == 64 ? 2 : 1) * (int64_t)device_info(dev).num_cu;
 }
 

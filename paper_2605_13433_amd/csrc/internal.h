@@ -49,6 +49,7 @@ enum CtrlSlot {
   CTRL_N_BWD = 5,       // entries in the combined backward list
   CTRL_STATUS = 6,      // seq_offsets contract status (HSTU_SEQ_* word)
   CTRL_N_PAIRS = 7,     // (sequence, query-tile pair) entries in the pair list
+  CTRL_N_FAR = 8,       // (sequence, chunk of query tiles) entries in the far list
   CTRL_WORDS = 64
 };
 
@@ -85,6 +86,10 @@ struct Problem {
   bool check_offsets;    // HSTU_VALIDATE=1: the scheduler checks the contract
   float alpha;           // scale of <q, k> (1 = plain operator)
   bool deterministic;    // backward: fixed-point table accumulation
+  // windowed operator: j is seen by i >= j if i - j < window or j < sinks (both in
+  // 0 .. N)
+  bool windowed = false;
+  int32_t window = 0, sinks = 0;
 };
 
 // Workspace carve-up; offsets in bytes from the workspace base, each region
@@ -96,7 +101,18 @@ struct Layout {
   int bwd_grid_both, bwd_grid_dq, bwd_grid_dkv;
   bool bwd_combined;
   int num_cu;                         // compute units of the device
+  // windowed bf16 backward: the far pass (0: none), see far_slot in attn_bf16_impl.h
+  int32_t far_chunk;                  // query tiles of a chunk
+  int32_t far_after;                  // the last query tile that the first key tile's
+                                      // windows reach
+  int64_t far_entries;                // most chunks of the batch
+  size_t list_f, far_part;
 };
+
+// Query tiles of a far chunk: long enough that a chunk's two float32 tiles are
+// little beside the rows it reads (a sixteenth of them for one sink tile), short
+// beside a sequence.
+constexpr int FAR_CHUNK = 16;
 
 // ---- host helpers shared by the C-ABI translation units ----
 // Records a formatted message as the thread's last error; returns `code`.
@@ -134,6 +150,9 @@ const DeviceInfo &device_info(int dev);
 
 Layout make_layout(const Problem &p, bool for_bwd, int dev);
 
+// Adds the window to a validated problem (`win` may be NULL: the causal operator).
+int set_window(const hstu_window *win, Problem *p);
+
 // A fixed device buffer that stands in for the caller's workspace: addr(dev)
 // returns its address on device `dev` (or nullptr after recording the
 // error), `bytes` its size.
@@ -146,8 +165,8 @@ struct FixedScratch {
 // caller's workspace (out->workspace), or, with `fixed`, on that buffer.
 int attn_fwd_call(const void *q, const void *k, const void *v, const void *u,
                   const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
-                  int32_t d, const hstu_rab *rab, hstu_fwd_out *out, void *stream,
-                  const FixedScratch *fixed);
+                  int32_t d, const hstu_rab *rab, const hstu_window *win, hstu_fwd_out *out,
+                  void *stream, const FixedScratch *fixed);
 
 
 // Form of the bf16 backward's dq, dk, dv, du outputs: rows of `stride`
@@ -164,8 +183,8 @@ struct GradOut {
 // backward, table finalize); `go` (bf16 only) sets the outputs' form.
 int attn_bwd_call(const void *q, const void *k, const void *v, const void *u,
                   const int64_t *seq_offsets, int32_t B, int32_t max_len, int32_t H,
-                  int32_t d, const hstu_rab *rab, hstu_bwd_io *io, void *stream,
-                  const GradOut *go);
+                  int32_t d, const hstu_rab *rab, const hstu_window *win, hstu_bwd_io *io,
+                  void *stream, const GradOut *go);
 
 // ---- launchers (each returns hipSuccess or the launch error) ----
 // Builds the work lists (and zeroes the d_time bins when the layout has
@@ -189,6 +208,18 @@ hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *o, bool direct, hipStre
 hipError_t launch_attn_bwd_bf16(const AttnArgs &a, const void *dO, void *dq, void *dk,
                                 void *dv, const GradOut *go, hipStream_t s);
 
+// One set of bf16 kernels' launchers (attn_bf16_impl.h); the windowed set.
+struct AttnBf16 {
+  bool (*direct_fits)(const Problem &p, int dev);
+  int (*bwd_grid)(const Problem &p, int dev);
+  int (*bwd_dq_grid)(const Problem &p, int dev);
+  int (*bwd_dkv_grid)(const Problem &p, int dev);
+  hipError_t (*fwd)(const AttnArgs &a, void *o, bool direct, hipStream_t s);
+  hipError_t (*bwd)(const AttnArgs &a, const void *dO, void *dq, void *dk, void *dv,
+                    const GradOut *go, hipStream_t s);
+};
+const AttnBf16 &attn_bf16_windowed();
+
 // The same for short batches (attn_short.hip) and the rules that choose it.
 bool fwd_short(const Problem &p, int dev);
 bool bwd_short(const Problem &p, int dev);
@@ -200,6 +231,11 @@ hipError_t launch_attn_fwd_f32(const AttnArgs &a, void *o, bool direct, hipStrea
 hipError_t launch_attn_bwd_f32(const AttnArgs &a, const void *dO, void *dq,
                                void *dk, void *dv, float *d_pos,
                                float *d_time, hipStream_t s);
+
+// Their windowed forms (attn_window_f32.hip).
+hipError_t launch_window_fwd_f32(const AttnArgs &a, void *o, bool direct, hipStream_t s);
+hipError_t launch_window_bwd_f32(const AttnArgs &a, const void *dO, void *dq, void *dk, void *dv,
+                                 float *d_pos, float *d_time, hipStream_t s);
 
 hipError_t launch_ln_fwd(const Problem &p, const void *o, const void *u,
                          void *y, float *mean, float *rstd, hipStream_t s);
@@ -242,7 +278,6 @@ constexpr int FWD_DIRECT_SEQS = 128;
 bool fwd_direct(const Problem &p, int dev);
 inline int64_t pair_entries(const Problem &p) { return (p.max_entries + p.B) / 2 + 1; }
 // Persistent-grid sizes (work-groups) of the bf16 attention kernels.
-int attn_fwd_grid(const Problem &p, int dev);
 int attn_bwd_grid(const Problem &p, int dev);
 int attn_bwd_dq_grid(const Problem &p, int dev);
 int attn_bwd_dkv_grid(const Problem &p, int dev);

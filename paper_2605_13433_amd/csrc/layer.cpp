@@ -452,7 +452,7 @@ int hstu_layer_bwd(const void *x, const void *w1, const void *w2,
                  io->d_pos_w, io->d_time_w, ws + L.attn, L.attn_bytes};
   const GradOut go{(int32_t)(4 * C), h + 2 * C, h + 3 * C, h + C, h};
   rc = attn_bwd_call(z + 2 * plane, z + 3 * plane, z + plane, z, seq_offsets, B, max_len, H,
-                     d, rab, &bo, stream, &go);
+                     d, rab, nullptr, &bo, stream, &go);
   if (rc != HSTU_OK || T == 0) return rc;
   // dx = dh . w1^T ;  dw1 = x^T . dh
   if ((rc = gemm(dev, rm(false, true, T, D, 4 * C, 4 * C, 4 * C, D), ws + L.dh,

@@ -60,6 +60,6 @@ extern "C" int hstu_jagged_attn_fwd_noalloc(const void *q, const void *k, const 
                                             const hstu_rab *rab, hstu_fwd_out *out,
                                             void *stream) {
   static const hstu::FixedScratch fixed{hstu::scratch_addr, hstu::SCRATCH_BYTES};
-  return hstu::attn_fwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, out, stream,
+  return hstu::attn_fwd_call(q, k, v, u, seq_offsets, B, max_len, H, d, rab, nullptr, out, stream,
                              &fixed);
 }

@@ -20,6 +20,9 @@
 //     pair of query tiles 2p, 2p+1 (the second past the sequence when
 //     ntiles_b is odd), cost ~ p+1; consumed by the bf16 forward's two-tile
 //     items.
+//   * far list (windowed backward calls): entries (b, t) for every chunk of
+//     far_chunk query tiles from t on that holds one which sees a sequence's first
+//     tokens alone of its first key tiles; consumed by the far items.
 //   * combined backward list: both kinds, dK/dV entries before dQ entries of
 //     equal cost (dQ entries flagged), consumed by the combined bf16
 //     backward kernel.  With `fuse_dq0` set, no sequence gets a dQ entry for
@@ -96,6 +99,8 @@ struct SchedArgs {
   int32_t check;                      // check the seq_offsets contract
   float *zero_out;
   int32_t n_zero;
+  WorkEntry *list_f;                  // far list (windowed backward), or NULL
+  int32_t far_chunk, far_after, cap_f;
 };
 
 // Runs in one work-group of NT threads.
@@ -178,6 +183,7 @@ __device__ __forceinline__ void build_schedule(const SchedArgs &a, SchedSmem &sm
       a.ctrl[CTRL_POP_DQ] = 0;
       a.ctrl[CTRL_POP_DKV] = 0;
       a.ctrl[CTRL_POP_BWD] = 0;
+      a.ctrl[CTRL_N_FAR] = 0;
       // every non-empty sequence (`ranks` of them) has one first q-tile
       const int32_t n_bwd = 2 * sm.total - (a.fuse_dq0 ? ranks : 0);
       a.ctrl[CTRL_N_BWD] = !run ? 0 : n_bwd < 2 * a.cap ? n_bwd : 2 * a.cap;
@@ -248,6 +254,13 @@ __device__ __forceinline__ void build_schedule(const SchedArgs &a, SchedSmem &sm
     const int sk = seq_major ? base + t : sm.cstart[ck] + r;
     if (sq < a.cap) a.list_q[sq] = we;
     if (a.list_k && sk < a.cap) a.list_k[sk] = we;
+    // far list: the chunks of query tiles that hold one past the first key tile's
+    // windows, in arbitrary order (equally long, and each has outputs of its own)
+    if (a.list_f && run && t % a.far_chunk == 0 &&
+        (t + a.far_chunk < nt ? t + a.far_chunk : nt) - 1 > a.far_after) {
+      const int sf = atomicAdd(&a.ctrl[CTRL_N_FAR], 1);
+      if (sf < a.cap_f) a.list_f[sf] = we;
+    }
     if (a.list_b) {
       // combined list: cost-major, bin c spans 2 ge(c) slots, its dK/dV
       // entries then its dQ entries; sequence-major, per sequence the
@@ -355,6 +368,10 @@ inline SchedArgs sched_args(const int64_t *seq_offsets, const Problem &p, void *
   a.zero_out = L.dtime_part ? (float *)(base + L.dtime_part) : nullptr;
   // 8 bytes per partial entry (see make_layout): DTIME_BINS histograms for
   // the bf16 backward, one table for the fp32 one
+  a.list_f = L.far_chunk ? (WorkEntry *)(base + L.list_f) : nullptr;
+  a.far_chunk = L.far_chunk;
+  a.far_after = L.far_after;
+  a.cap_f = (int32_t)L.far_entries;
   a.n_zero = L.dtime_part ? 2 * (p.dtype == HSTU_BF16 ? DTIME_BINS : 1) * p.H * p.nb : 0;
   return a;
 }

@@ -44,6 +44,10 @@ class Rab(ctypes.Structure):
                 ("alpha", ctypes.c_float)]
 
 
+class Window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
 class FwdOut(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int), ("total_tokens", ctypes.c_int64),
                 ("y", ctypes.c_void_p), ("o", ctypes.c_void_p),
@@ -111,6 +115,17 @@ def load_library(path: str = LIB_PATH):
     lib.hstu_jagged_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i64, i32,
                                                      ctypes.c_int, ctypes.POINTER(Rab)]
     lib.hstu_jagged_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.hstu_jagged_window_attn_fwd.argtypes = [P, P, P, P, P, i32, i32, i32, i32,
+                                                ctypes.POINTER(Rab), ctypes.POINTER(Window),
+                                                ctypes.POINTER(FwdOut), P]
+    lib.hstu_jagged_window_attn_fwd.restype = ctypes.c_int
+    lib.hstu_jagged_window_attn_bwd.argtypes = [P, P, P, P, P, i32, i32, i32, i32,
+                                                ctypes.POINTER(Rab), ctypes.POINTER(Window),
+                                                ctypes.POINTER(BwdIO), P]
+    lib.hstu_jagged_window_attn_bwd.restype = ctypes.c_int
+    lib.hstu_jagged_window_attn_workspace_bytes.argtypes = [
+        i32, i32, i32, i32, i64, i32, ctypes.c_int, ctypes.POINTER(Rab), ctypes.POINTER(Window)]
+    lib.hstu_jagged_window_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.hstu_jagged_schedule.argtypes = [P, i32, i32, i64, P, P, P, P, ctypes.c_size_t, P]
     lib.hstu_jagged_schedule.restype = ctypes.c_int
     lib.hstu_layer_fwd.argtypes = [P, P, P, P, i32, i32, i32, i32, i32,
@@ -220,6 +235,41 @@ def hstu_jagged_attn_bwd(q, k, v, u, seq_offsets, B, max_len, H, d,
         _ptr(q), _ptr(k), _ptr(v), _ptr(u), _ptr(seq_offsets), int(B),
         int(max_len), int(H), int(d), ctypes.byref(rab) if rab is not None else None,
         ctypes.byref(io), _stream(stream)))
+
+
+def make_window(window, sinks=0) -> Optional[Window]:
+    """None without a window (the plain operator)."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks are given without a window")
+        return None
+    return Window(int(window), int(sinks))
+
+
+def hstu_jagged_window_attn_workspace_bytes(B, max_len, H, d, total_tokens, for_bwd, dtype_code,
+                                            rab: Optional[Rab], win: Window) -> int:
+    n = load_library().hstu_jagged_window_attn_workspace_bytes(
+        int(B), int(max_len), int(H), int(d), int(total_tokens), int(for_bwd),
+        int(dtype_code), ctypes.byref(rab) if rab is not None else None, ctypes.byref(win))
+    if n == 0:
+        raise HstuError(-1, last_error())
+    return n
+
+
+def hstu_jagged_window_attn_fwd(q, k, v, u, seq_offsets, B, max_len, H, d, rab: Optional[Rab],
+                                win: Window, out: FwdOut, stream=None) -> None:
+    _check(load_library().hstu_jagged_window_attn_fwd(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(u), _ptr(seq_offsets), int(B),
+        int(max_len), int(H), int(d), ctypes.byref(rab) if rab is not None else None,
+        ctypes.byref(win), ctypes.byref(out), _stream(stream)))
+
+
+def hstu_jagged_window_attn_bwd(q, k, v, u, seq_offsets, B, max_len, H, d, rab: Optional[Rab],
+                                win: Window, io: BwdIO, stream=None) -> None:
+    _check(load_library().hstu_jagged_window_attn_bwd(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(u), _ptr(seq_offsets), int(B),
+        int(max_len), int(H), int(d), ctypes.byref(rab) if rab is not None else None,
+        ctypes.byref(win), ctypes.byref(io), _stream(stream)))
 
 
 def hstu_jagged_schedule(seq_offsets, B, max_len, total_tokens, n_entries, list_q,
@@ -367,20 +417,22 @@ def _workspace(nbytes: int, device) -> torch.Tensor:
 
 
 class Plan:
-    """Outputs + workspace for one problem shape, allocated once and reused."""
+    """Outputs + workspace for one problem shape, allocated once and reused.
+    With `window`, a token sees its `window` most recent tokens (itself among
+    them) and the first `sinks` tokens of its sequence."""
 
     def __init__(self, q, seq_offsets, max_len, pos_w=None, time_w=None,
                  timestamps=None, num_buckets=128, backward=True, alpha=1.0,
-                 deterministic=False):
+                 deterministic=False, window=None, sinks=0):
         T, H, d = q.shape
         dev = q.device
         self.B = seq_offsets.numel() - 1
         self.N, self.H, self.d, self.T = int(max_len), H, d, T
         self.rab = make_rab(pos_w, time_w, timestamps, num_buckets, alpha)
+        self.win = make_window(window, sinks)
         self._keep = (pos_w, time_w, timestamps)
         code = _dtype_code(q)
-        self.fwd_ws = _workspace(hstu_jagged_attn_workspace_bytes(
-            self.B, self.N, H, d, T, 0, code, self.rab), dev)
+        self.fwd_ws = _workspace(self._workspace_bytes(0, code), dev)
         self.y = torch.empty(T, H * d, dtype=q.dtype, device=dev)
         self.o = torch.empty(T, H, d, dtype=q.dtype, device=dev)
         self.mean = torch.empty(T, dtype=torch.float32, device=dev)
@@ -389,8 +441,7 @@ class Plan:
                           _ptr(self.rstd), _ptr(self.fwd_ws), self.fwd_ws.numel())
         self.io = None
         if backward:
-            self.bwd_ws = _workspace(hstu_jagged_attn_workspace_bytes(
-                self.B, self.N, H, d, T, 1, code, self.rab), dev)
+            self.bwd_ws = _workspace(self._workspace_bytes(1, code), dev)
             self.dq = torch.empty(T, H, d, dtype=q.dtype, device=dev)
             self.dk = torch.empty_like(self.dq)
             self.dv = torch.empty_like(self.dq)
@@ -404,6 +455,12 @@ class Plan:
                             _ptr(self.d_pos), _ptr(self.d_time), _ptr(self.bwd_ws),
                             self.bwd_ws.numel(), 1 if deterministic else 0)
 
+    def _workspace_bytes(self, for_bwd, code) -> int:
+        size = (self.B, self.N, self.H, self.d, self.T, for_bwd, code, self.rab)
+        if self.win is None:
+            return hstu_jagged_attn_workspace_bytes(*size)
+        return hstu_jagged_window_attn_workspace_bytes(*size, self.win)
+
     def status(self, backward=False, stream=None) -> int:
         """The seq_offsets status word (HSTU_SEQ_* bits) of the last forward
         (or backward) call; waits for the stream."""
@@ -412,29 +469,38 @@ class Plan:
         return int(st.item())
 
     def forward(self, q, k, v, u, seq_offsets, stream=None) -> FwdResult:
-        hstu_jagged_attn_fwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
-                             self.rab, self.out, stream)
+        if self.win is None:
+            hstu_jagged_attn_fwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
+                                 self.rab, self.out, stream)
+        else:
+            hstu_jagged_window_attn_fwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
+                                        self.rab, self.win, self.out, stream)
         return FwdResult(self.y, self.o, self.mean, self.rstd)
 
     def backward(self, q, k, v, u, seq_offsets, dy, stream=None) -> BwdResult:
         self.io.dy = _ptr(dy)
         self._dy = dy
-        hstu_jagged_attn_bwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
-                             self.rab, self.io, stream)
+        if self.win is None:
+            hstu_jagged_attn_bwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
+                                 self.rab, self.io, stream)
+        else:
+            hstu_jagged_window_attn_bwd(q, k, v, u, seq_offsets, self.B, self.N, self.H, self.d,
+                                        self.rab, self.win, self.io, stream)
         return BwdResult(self.dq, self.dk, self.dv, self.du, self.d_pos, self.d_time)
 
 
 def forward(q, k, v, u, seq_offsets, max_len, pos_w=None, time_w=None,
-            timestamps=None, num_buckets=128, alpha=1.0) -> FwdResult:
+            timestamps=None, num_buckets=128, alpha=1.0, window=None, sinks=0) -> FwdResult:
     plan = Plan(q, seq_offsets, max_len, pos_w, time_w, timestamps, num_buckets,
-                backward=False, alpha=alpha)
+                backward=False, alpha=alpha, window=window, sinks=sinks)
     return plan.forward(q, k, v, u, seq_offsets)
 
 
 def forward_backward(q, k, v, u, seq_offsets, max_len, dy, pos_w=None, time_w=None,
-                     timestamps=None, num_buckets=128, alpha=1.0, deterministic=False):
+                     timestamps=None, num_buckets=128, alpha=1.0, deterministic=False,
+                     window=None, sinks=0):
     plan = Plan(q, seq_offsets, max_len, pos_w, time_w, timestamps, num_buckets,
-                alpha=alpha, deterministic=deterministic)
+                alpha=alpha, deterministic=deterministic, window=window, sinks=sinks)
     f = plan.forward(q, k, v, u, seq_offsets)
     g = plan.backward(q, k, v, u, seq_offsets, dy)
     return f, g
