@@ -2,7 +2,8 @@
 
 Submodules:
   hstu    ctypes binding of include/hstu_jagged.h (loads libhstu_jagged.so)
+  paged   ctypes binding of include/hstu_cache.h (paged cache, one-token attention)
   inputs  seeded synthetic workloads (no attention arithmetic)
   build   compiles the HIP library in-tree
 """
-__all__ = ["hstu", "inputs", "build"]
+__all__ = ["hstu", "paged", "inputs", "build"]

@@ -19,9 +19,9 @@ LIB = os.path.join(HERE, "libhstu_jagged.so")
 ARCH = "gfx950"
 SOURCES = ["api.cpp", "sched.hip", "attn_bf16.hip", "attn_window.hip", "attn_short.hip",
            "attn_f32.hip", "attn_window_f32.hip", "norm.hip", "layer.cpp", "layer_kernels.hip",
-           "noalloc.hip", "embedding.hip", "rab.hip", "gemm.hip"]
+           "noalloc.hip", "embedding.hip", "rab.hip", "gemm.hip", "cache.hip", "paged_attn.hip"]
 HEADERS = ["device.h", "internal.h", "sched_impl.h", "attn_common.h", "attn_bf16_impl.h",
-           "attn_f32_impl.h"]
+           "attn_f32_impl.h", "cache.h", "cache_index.h"]
 
 CFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
