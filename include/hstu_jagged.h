@@ -209,14 +209,24 @@ size_t hstu_jagged_attn_workspace_bytes(int32_t B, int32_t max_len, int32_t H,
  * reaches only rows that see it or are seen by it (and the table entries of such
  * pairs).
  *
+ * Bias tables in HSTU_BF16.  A table's gradient is a sum over many pairs whose signs
+ * differ, in which the roundings of a, o and dO to bf16 would stay (2e-3 of it, as in
+ * the plain call).  With a table, the forward therefore also hands o on in float32
+ * (o_full, which LayerNorm then reads), and the backward carries dO to 24 bits: the
+ * table gradients are as exact as those of HSTU_F32.
+ *
  * Work and memory grow with total_tokens x (window + sinks).  The backward of
- * HSTU_BF16 takes a further workspace for the sinks' gradients over the queries
- * past their windows, at most a quarter of q's size and 2 x 64 x d x H floats per
+ * HSTU_BF16 takes a further workspace, twice q's size with a bias table (dO's further
+ * bits), and for the sinks' gradients over the queries past their windows at most a quarter of q's size and 2 x 64 x d x H floats per
  * sequence and 64 sinks.
  * ------------------------------------------------------------------------- */
 typedef struct {
     int32_t window;              /* >= 0                                     */
     int32_t sinks;               /* >= 0                                     */
+    float *o_full;               /* HSTU_BF16 with a bias table: [T][H][d], o
+                                    before its rounding; written by the forward
+                                    unless NULL, needed by the backward.  Not
+                                    used otherwise                          */
 } hstu_window;
 
 size_t hstu_jagged_window_attn_workspace_bytes(int32_t B, int32_t max_len,

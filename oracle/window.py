@@ -51,12 +51,9 @@ def _layer_norm(o):
 
 
 def attention(q, k, v, u, off, N, window, sinks, pos_w=None, time_w=None, ts=None, dy=None,
-              alpha=1.0, noise=False):
+              alpha=1.0):
     """q, k, v, u, dy [T][H][d] (u, dy also [T][H*d]; any float type), off [B+1]; the outputs
-    of the forward, and with dy of the backward, by name.  With `noise`, also
-    d_pos_noise and d_time_noise: the root of the summed squares of dO_c v_c times
-    silu' / N over an entry's pairs, by which the entry's standard error follows
-    from the relative one of dO's elements."""
+    of the forward, and with dy of the backward, by name."""
     f = lambda x: None if x is None else np.asarray(x, dtype=np.float64)
     q, k, v, u, dy, pos_w, time_w = map(f, (q, k, v, u, dy, pos_w, time_w))
     T, H, d = q.shape
@@ -86,8 +83,6 @@ def attention(q, k, v, u, off, N, window, sinks, pos_w=None, time_w=None, ts=Non
                dv=np.zeros((T, H, d)),
                d_pos=None if pos_w is None else np.zeros_like(pos_w),
                d_time=None if time_w is None else np.zeros_like(time_w))
-    pos_var = None if pos_w is None else np.zeros_like(pos_w)
-    time_var = None if time_w is None else np.zeros_like(time_w)
     for b in range(len(off) - 1):
         r = slice(int(off[b]), int(off[b + 1]))
         L = r.stop - r.start
@@ -104,20 +99,10 @@ def attention(q, k, v, u, off, N, window, sinks, pos_w=None, time_w=None, ts=Non
             out["dq"][r, h] = alpha * ds @ k[r, h]
             out["dk"][r, h] = alpha * ds.T @ q[r, h]
             out["dv"][r, h] = a.T @ dO[r, h]
-            if noise:
-                f2 = np.where(m, sg * (1.0 + s * (1.0 - sg)) / N, 0.0) ** 2
-                var = f2 * (dO[r, h] ** 2 @ (v[r, h] ** 2).T)
-                if pos_w is not None:
-                    np.add.at(pos_var[h], np.broadcast_to(j - i + N - 1, (L, L)), var)
-                if time_w is not None:
-                    np.add.at(time_var[h], bucket(t[i] - t[j], time_w.shape[1]), var)
             if pos_w is not None:
                 np.add.at(out["d_pos"][h], np.broadcast_to(j - i + N - 1, (L, L)), ds)
             if time_w is not None:
                 np.add.at(out["d_time"][h], bucket(t[i] - t[j], time_w.shape[1]), ds)
-    if noise:
-        out["d_pos_noise"] = None if pos_w is None else np.sqrt(pos_var)
-        out["d_time_noise"] = None if time_w is None else np.sqrt(time_var)
     return out
 
 

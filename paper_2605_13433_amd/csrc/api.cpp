@@ -95,6 +95,7 @@ int set_window(const hstu_window *win, Problem *p) {
   p->windowed = true;
   p->window = std::min(win->window, p->N);
   p->sinks = std::min(win->sinks, p->N);
+  p->exact = p->dtype == HSTU_BF16 && (p->has_pos || p->has_time) && win->o_full;
   return HSTU_OK;
 }
 
@@ -202,6 +203,10 @@ Layout make_layout(const Problem &p, bool for_bwd, int dev) {
   L.list_p = !for_bwd && fwd_pairs(p) ? take(sizeof(WorkEntry) * (size_t)pair_entries(p)) : 0;
   L.dO = for_bwd ? take(elem * (size_t)p.T * p.H * p.d) : 0;
   const bool bf16_bwd = for_bwd && p.dtype == HSTU_BF16;
+  if (bf16_bwd && p.windowed && (p.has_pos || p.has_time)) {
+    L.dO_mid = take(elem * (size_t)p.T * p.H * p.d);
+    L.dO_low = take(elem * (size_t)p.T * p.H * p.d);
+  }
   L.num_cu = device_info(dev).num_cu;
   L.bwd_grid_both = bf16_bwd ? attn_bwd_grid(p, dev) : 0;
   L.bwd_grid_dq = bf16_bwd ? attn_bwd_dq_grid(p, dev) : 0;
@@ -277,7 +282,7 @@ int attn_fwd_call(const void *q, const void *k, const void *v, const void *u,
              rab ? rab->pos_w : nullptr,
              p.has_time ? rab->time_w : nullptr,
              p.has_time ? rab->timestamps : nullptr,
-             ws, L, p};
+             ws, L, p, p.exact ? win->o_full : nullptr};
   // the no-allocation path never records profiler events (creating one may
   // allocate)
   const bool prof_on = !fixed;
@@ -298,7 +303,7 @@ int attn_fwd_call(const void *q, const void *k, const void *v, const void *u,
   if (e != hipSuccess) return hip_fail(e, "attention forward launch");
   {
     prof::Scope ps(prof_on ? "ln_fwd" : nullptr, s);
-    e = launch_ln_fwd(p, out->o, u, out->y, out->ln_mean, out->ln_rstd, s);
+    e = launch_ln_fwd(p, out->o, a.o_full, u, out->y, out->ln_mean, out->ln_rstd, s);
   }
   if (e != hipSuccess) return hip_fail(e, "layernorm forward launch");
   return HSTU_OK;
@@ -323,6 +328,8 @@ int attn_bwd_call(const void *q, const void *k, const void *v, const void *u,
     return fail(HSTU_EINVAL, "rab->pos_w given but io->d_pos_w is NULL");
   if (p.has_time && !io->d_time_w)
     return fail(HSTU_EINVAL, "rab->time_w given but io->d_time_w is NULL");
+  if (p.T > 0 && p.windowed && p.dtype == HSTU_BF16 && (p.has_pos || p.has_time) && !p.exact)
+    return fail(HSTU_EINVAL, "a bias table given but win->o_full is NULL");
   if (p.T == 0 && !p.has_pos && !p.has_time) return HSTU_OK;
   p.deterministic = io->deterministic != 0;
   int dev = 0;
@@ -343,7 +350,7 @@ int attn_bwd_call(const void *q, const void *k, const void *v, const void *u,
   if (p.T > 0) {
     // the LayerNorm backward launch also builds the work lists
     prof::Scope ps("ln_bwd", s);
-    e = launch_ln_bwd_sched(p, io->dy, u, io->o, io->ln_mean, io->ln_rstd, io->du,
+    e = launch_ln_bwd_sched(p, io->dy, u, io->o, win ? win->o_full : nullptr, io->ln_mean, io->ln_rstd, io->du,
                             ws + L.dO,
                             (L.dpos_part && p.dtype == HSTU_BF16) ? ws + L.dpos_part : nullptr,
                             seq_offsets, ws, L, go, s);

@@ -112,6 +112,8 @@ struct KParams {
   int32_t far_chunk;      // query tiles of a far item (0: no far pass)
   int32_t far_slots;      // capacity of far_part, in partial tiles per head
   float *far_part;        // far items' dK and dV sums (see far_slot)
+  const u16 *dO_mid, *dO_low;   // the rest of dO (see "exact tables")
+  float *o_full;          // forward: o before its rounding, or NULL
 };
 
 // Stationary 32-row operand: lane holds row `row` of the tile (zero when
@@ -308,6 +310,32 @@ __device__ __forceinline__ int last_query_tile(const KParams &P, int kt, int nti
   int e = t < ntiles - 1 ? (int)t : ntiles - 1;
   if (P.far_chunk == 0 && kt * TILE < P.sinks) e = ntiles - 1;
   return max(e, kt);
+}
+
+// Exact tables.  The gradient of a bias table is a float32 sum of dS over many pairs
+// whose signs differ, so what dS loses stays in it: the roundings of A, o and dO to
+// bf16 leave 2e-3 of a table.  With a table, the windowed operator carries those three
+// as sums of bf16 parts, which the matrix cores multiply one after the other: A and dO
+// in three parts (24 bits: the float's own), o in float32 beside its rounded form.  The
+// forward then has three products for O instead of one (attn_fwd_kernel with EXACT),
+// the dQ items three for dA, and the tables are summed in the dQ items; dK and dV, which
+// are rounded to bf16 anyway, use dO's first part alone.  Error of the tables against
+// 64 bits 2e-3 -> 4e-7 (window_train figures in the launch section).
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&part)[3]) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pack2(r[2 * e], r[2 * e + 1]);
+      r[2 * e] -= __uint_as_float(w[e] << 16);
+      r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+    }
+    part[p] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+  }
 }
 
 // Far items.  A sink tile is seen by every later query of its sequence, a chain as
@@ -755,7 +783,7 @@ __device__ __forceinline__ void fwd_item_start(const KParams &P, const Item &it,
 // Cross-wave sum of the O tile of one query tile (waves with `mine` set, in
 // two key halves: `writer` stores, its partner adds) and its coalesced bf16
 // store by all NT threads; rows at or beyond `valid` are not written.
-template <int D, int NT, bool WIN>
+template <int D, int NT, bool WIN, bool EXACT>
 __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, float *red, const f32x16 (&acc)[D / 32], bool mine,
                                             bool writer, int half, int g, int l32, int tid,
                                             u16 *__restrict__ out, int row_stride, int valid) {
@@ -786,6 +814,11 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, 
       const float4 b = *(const float4 *)(red + row * D + 8 * c8 + 4);
       float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
       if constexpr (WIN) finish_chunk<D, Sum::O>(P, ro, row, c8, f);
+      if constexpr (EXACT) {
+        float *full = P.o_full + (out - P.out0) + (int64_t)row * row_stride + 8 * c8;
+        *(float4 *)full = make_float4(f[0], f[1], f[2], f[3]);
+        *(float4 *)(full + 4) = make_float4(f[4], f[5], f[6], f[7]);
+      }
       uint4 pk;
       pk.x = pack2(f[0], f[1]);
       pk.y = pack2(f[2], f[3]);
@@ -815,7 +848,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, 
 // item's last tile streams the next item's first key tile, query rows, bias
 // slice and timestamps, so no item starts with an exposed memory latency.
 // DIRECT: one item per work-group, found from the offsets (fwd_direct).
-template <int D, bool POS, bool TIME, int QT, bool DIRECT, bool WIN>
+template <int D, bool POS, bool TIME, int QT, bool DIRECT, bool WIN, bool EXACT>
 __global__ void __launch_bounds__(THREADS * QT, QT == 1 ? 2 : 1)
 attn_fwd_kernel(KParams P) {
   static_assert(QT == 1 || !DIRECT, "direct items are one query tile");
@@ -1065,6 +1098,20 @@ attn_fwd_kernel(KParams P) {
           for (int e = 0; e < 8; ++e)
             if (hidden<WIN>(P, qt, kt, i_loc, kb + c_row(8 * hh + e, 0))) av[e] = 0.0f;
         }
+        if constexpr (EXACT) {
+          bf16x8 pa[3];
+          split8(av, pa);
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) {
+            const bf16x8 vt = sread_tr_at(vt_lds, voff[db] + hh * 16 * D * 2,
+                                          (V_HI ? vofh[V_HI ? db : 0] : voff[db] + 8 * D * 2) +
+                                              hh * 16 * D * 2);
+            oacc[db] = mfma32(pa[2], vt, oacc[db]);
+            oacc[db] = mfma32(pa[1], vt, oacc[db]);
+            oacc[db] = mfma32(pa[0], vt, oacc[db]);
+          }
+          continue;
+        }
         uint4 pk;
         pk.x = pack2(av[0], av[1]);
         pk.y = pack2(av[2], av[3]);
@@ -1089,7 +1136,7 @@ attn_fwd_kernel(KParams P) {
     for (int sq = 0; sq < QT; ++sq) {
       const int tq = QT * it.tile + sq;
       const RowsOf ro{it.start, it.len, h, tq, 0, nullptr, 0};
-      fwd_store_o<D, NT, WIN>(P, ro, (float *)sm.tile[(phase - 1) & 1], oacc, sub == sq, wj == 0, wi, g,
+      fwd_store_o<D, NT, WIN, EXACT>(P, ro, (float *)sm.tile[(phase - 1) & 1], oacc, sub == sq, wj == 0, wi, g,
                          l32, tid, P.out0 + ((it.start + (int64_t)tq * TILE) * P.H + h) * D,
                          row_stride, it.len - tq * TILE);
     }
@@ -1209,12 +1256,52 @@ __device__ __forceinline__ SeqInfo entry_seq(const WorkEntry &e) {
 }
 
 // --------------------------------------------------------------------- dQ
+// What a windowed dQ item needs for the tables ("exact tables"): the LDS tiles of dO's
+// second and third part (d = 128; at d = 64 they are registers), the diagonal windows
+// and the time histogram.
+template <bool DET>
+struct TabRefs {
+  u16 *mid, *low;
+  typename TabAcc<DET>::L (*pwin)[2][2 * TILE];         // [window][lane group][slot]
+  typename TabAcc<DET>::L *hist;
+};
+
+// As dpos_retire, for a dQ item, whose tile offset dt = qt - kt falls from step to
+// step: slots x >= 63 of the finished window are final, the others carry into slot
+// x + 64 of the current one -- or all are final, after the last step and before a step
+// over the tiles that are not seen.
+template <typename A>
+__device__ __forceinline__ void dpos_retire_q(typename A::L (*prev)[2 * TILE],
+                                              typename A::L (*cur)[2 * TILE], int x, int dt,
+                                              bool last, int len, typename A::G *dp, int H) {
+  const typename A::L v = prev[0][x] + prev[1][x];
+  prev[0][x] = 0;
+  prev[1][x] = 0;
+  if (v == 0) return;
+  const int m = dt * TILE + x - (TILE - 1);
+  if (x >= TILE - 1 || last) {
+    if (m >= 0 && m < len) atomicAdd(dp + m * H, A::glob(v));
+  } else {
+    atomicAdd(&cur[0][x + TILE], v);
+  }
+}
+
+// d_time sums of `heads` heads from `h0` on, out of the LDS histogram into one of
+// DTIME_BINS partial tables; the counters are cleared.
+template <bool DET>
+__device__ __forceinline__ void time_fold(const KParams &P, typename TabAcc<DET>::L *tacc,
+                                          int tid, int h0, int heads);
+
 // One q-stationary item: dQ_i = sum_{j<=i} dS_ij k_j for a 64-row query tile
 // of one head, recomputing S and dA = dO V^T tile by tile.
-template <int D, bool POS, bool TIME, bool WIN>
-__device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, float *dyn,
+template <int D, bool POS, bool TIME, bool WIN, bool DET>
+__device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
+                                        const TabRefs<DET> &tab, float *dyn,
                                         const int tid0, const WorkEntry e, const int h,
                                         int &phase, int &nxt) {
+  typedef TabAcc<DET> A;
+  constexpr bool TAB = WIN && (POS || TIME);
+  constexpr bool TAB_LDS = TAB && D == 128;       // dO's second and third part
   constexpr int ST = D + RM_PAD;
     int tid = tid0;
     asm volatile("" : "+v"(tid));
@@ -1238,6 +1325,16 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
     bf16x8 qreg[D / 16], doreg[D / 16];
     load_stationary<D>(P.q + qoff, i_loc, q_valid, row_stride, g, qreg);
     load_stationary<D>(P.dO + qoff, i_loc, q_valid, row_stride, g, doreg);
+    bf16x8 midreg[TAB && !TAB_LDS ? D / 16 : 1], lowreg[TAB && !TAB_LDS ? D / 16 : 1];
+    if constexpr (TAB_LDS) {
+      int ln = lane;                       // (as the dK/dV item's stationary tiles)
+      asm volatile("" : "+v"(ln));
+      dma_tile<D, SWZ_CF>(P.dO_mid + qoff, q_valid, row_stride, tab.mid, w, ln);
+      dma_tile<D, SWZ_CF>(P.dO_low + qoff, q_valid, row_stride, tab.low, w, ln);
+    } else if constexpr (TAB) {
+      load_stationary<D>(P.dO_mid + qoff, i_loc, q_valid, row_stride, g, midreg);
+      load_stationary<D>(P.dO_low + qoff, i_loc, q_valid, row_stride, g, lowreg);
+    }
     // the sequence's K and V rows of head h, each one source for the item
     const uint32_t seq_bytes = 2u * (uint32_t)si.len * (uint32_t)row_stride;
     const __amdgpu_buffer_rsrc_t rs_k = make_rsrc(P.k + (si.start * P.H + h) * D, seq_bytes);
@@ -1277,12 +1374,25 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[db][r] = 0.0f;
 
-    for (int kt = k0; kt <= qt; kt = keys.next(kt), ++phase) {
+    TimeRun<A> run;
+    typename A::L *my_t = nullptr;
+    typename A::G *dp_item = nullptr;
+    if constexpr (TAB && TIME) my_t = tab.hist + h * P.time_hs + (lane & ((1 << P.time_cs) - 1));
+    if constexpr (TAB && POS) dp_item = (typename A::G *)P.dpos_part + si.start * P.H + h;
+    if constexpr (TAB_LDS) wait_vm();         // the first step's barriers publish the tiles
+    int kp = k0;                              // the step before's tile
+
+    for (int kt = k0; kt <= qt; kp = kt, kt = keys.next(kt), ++phase) {
       const int kn = keys.next(kt);
       lds_barrier();
       kr.store(sm.t.a, tid);
       vr.store(sm.t.b, tid);
       if (POS) pos_store<false>(pos_v, P.inv_alpha, sm.pos, tid);
+      if constexpr (TAB && POS) {
+        if (kt != k0 && tid < 2 * TILE - 1)
+          dpos_retire_q<A>(tab.pwin[(phase - 1) & 1], tab.pwin[phase & 1], tid, qt - kp,
+                           kt != kp + 1, si.len, dp_item, P.H);
+      }
       if (TIME) {
         bool far = q_far;
         if (tid < TILE) {
@@ -1331,14 +1441,24 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         s = mfma32(read_rm(sm.t.a, ST, 32 * wj + l32, 16 * ks + 8 * g), qreg[ks], s);
-        da = mfma32(read_rm(sm.t.b, ST, 32 * wj + l32, 16 * ks + 8 * g), doreg[ks], da);
+        const bf16x8 vrow = read_rm(sm.t.b, ST, 32 * wj + l32, 16 * ks + 8 * g);
+        da = mfma32(vrow, doreg[ks], da);
+        if constexpr (TAB_LDS) {
+          da = mfma32(vrow, sread_rm<D, SWZ_CF>(tab.mid, i_loc, 16 * ks + 8 * g), da);
+          da = mfma32(vrow, sread_rm<D, SWZ_CF>(tab.low, i_loc, 16 * ks + 8 * g), da);
+        } else if constexpr (TAB) {
+          da = mfma32(vrow, midreg[ks], da);
+          da = mfma32(vrow, lowreg[ks], da);
+        }
       }
 
       // dS = dA silu'(x), then dQ += dS K, one 16-key half at a time (half the
       // temporaries live at once)
+      float carry = 0.0f;       // d_pos: a quad's row-head sums for the next quad
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
         float x[8], sg[8], dsv[8];
+        int tk[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[8 * hh + e];
         if (TIME) {
@@ -1346,15 +1466,21 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
               const float4 t4 = *(const float4 *)(sm.ts32 + kb + 8 * (2 * hh + q));
-              x[4 * q + 0] += ktab[time_index(ts_i32 - t4.x)];
-              x[4 * q + 1] += ktab[time_index(ts_i32 - t4.y)];
-              x[4 * q + 2] += ktab[time_index(ts_i32 - t4.z)];
-              x[4 * q + 3] += ktab[time_index(ts_i32 - t4.w)];
+              tk[4 * q + 0] = time_index(ts_i32 - t4.x);
+              tk[4 * q + 1] = time_index(ts_i32 - t4.y);
+              tk[4 * q + 2] = time_index(ts_i32 - t4.z);
+              tk[4 * q + 3] = time_index(ts_i32 - t4.w);
+              x[4 * q + 0] += ktab[tk[4 * q + 0]];
+              x[4 * q + 1] += ktab[tk[4 * q + 1]];
+              x[4 * q + 2] += ktab[tk[4 * q + 2]];
+              x[4 * q + 3] += ktab[tk[4 * q + 3]];
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              x[e] += ktab[KTAB + time_bucket(ts_i - sm.ts64[kb + c_row(8 * hh + e, 0)], P.nb)];
+            for (int e = 0; e < 8; ++e) {
+              tk[e] = time_bucket(ts_i - sm.ts64[kb + c_row(8 * hh + e, 0)], P.nb);
+              x[e] += ktab[KTAB + tk[e]];
+            }
           }
         }
         // the score is alpha x: sigma(alpha x)
@@ -1370,6 +1496,42 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
           for (int e = 0; e < 8; ++e)
             if (hidden<WIN>(P, qt, kt, i_loc, kb + c_row(8 * hh + e, 0))) dsv[e] = 0.0f;
         }
+        if constexpr (TAB && POS) {
+          // as the dK/dV item's (see there): element (i, j) -> slot i_loc - j_loc + 63,
+          // here with the lane's row the query and the quads' rows the keys j0 .. j0+3;
+          // element j0 + k of lane l+k lies on the diagonal of element j0 of lane l
+          typename A::L *pw = &tab.pwin[phase & 1][g][i_loc - kb + (TILE - 1)];
+          const bool row_head = (lane & 15) < 3;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float *v = dsv + 4 * q;
+            const float b4 =
+                ((v[0] + row_shl<1>(v[1])) + row_shl<2>(v[2])) + row_shl<3>(v[3]);
+            const float band = hh == 0 && q == 0 ? b4 : b4 + carry;   // first quad: none
+            const float head = (v[3] + row_shr<1>(v[2])) + row_shr<2>(v[1]);
+            const int at = 16 * hh + 8 * q;             // c_row(8 hh + 4 q, 0)
+            atomicAdd(pw - at, A::lds(L2E * band));
+            if (hh == 1 && q == 1) {
+              if (row_head) atomicAdd(pw - at - 3, A::lds(L2E * head));
+            } else {
+              carry = row_shr<5>(row_head ? head : 0.0f);
+            }
+          }
+        }
+        if constexpr (TAB && TIME) {
+          if (!slow) {
+            if (hh == 0) run.start(tk[0]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) run.add(my_t, P.nb, P.time_cs, tk[e], L2E * dsv[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float v = L2E * dsv[e];
+              asm volatile("" : "+v"(v));       // (as in the dK/dV item)
+              if (v != 0.0f) atomicAdd(&my_t[tk[e] << P.time_cs], A::lds(v));
+            }
+          }
+        }
         uint4 pk;
         pk.x = pack2(dsv[0], dsv[1]);
         pk.y = pack2(dsv[2], dsv[3]);
@@ -1384,6 +1546,16 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm, flo
     }
 
     if (D != 64 && fuse) kr.load(P.h_dq + ooff, q_valid, P.out_stride, tid);
+    if constexpr (TAB) {
+      if constexpr (TIME) run.flush(my_t, P.nb, P.time_cs);
+      lds_barrier();
+      if (TIME && P.time_hs == 0) time_fold<DET>(P, tab.hist, tid, h, 1);
+      if constexpr (POS) {   // every diagonal of the last window is final
+        if (tid < 2 * TILE - 1)
+          dpos_retire_q<A>(tab.pwin[(phase - 1) & 1], tab.pwin[phase & 1], tid, 0, true, si.len,
+                           dp_item, P.H);
+      }
+    }
     const RowsOf ro{si.start, si.len, h, qt, 0, nullptr, 0};
     sum_store_tile<D, WIN, Sum::DQ>(P, ro, &sm.red[0][0], acc, wj == 0, wi, g, l32, tid,
                                     P.dq_out + ooff, P.out_stride, q_valid, P.dqk_scale, fuse,
@@ -1457,8 +1629,6 @@ __device__ __forceinline__ f32x16 dq0_block(const u16 *dsb, const u16 *kst, int 
   return dq;
 }
 
-// d_time sums of `heads` heads from `h0` on, out of the LDS histogram into one of
-// DTIME_BINS partial tables; the counters are cleared.
 template <bool DET>
 __device__ __forceinline__ void time_fold(const KParams &P, typename TabAcc<DET>::L *tacc,
                                           int tid, int h0, int heads) {
@@ -1491,6 +1661,8 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
                                          u16 *dsb = nullptr, int far_q0 = 0, int far_q1 = 0,
                                          float *far = nullptr) {
   typedef TabAcc<DET> A;
+  // the windowed operator's tables are the dQ items' ("exact tables")
+  constexpr bool POS_T = POS && !WIN, TIME_T = TIME && !WIN;
   constexpr int ST = D + RM_PAD;
   StreamSmem<D> &sm = smx.s;
     int tid = tid0;
@@ -1567,8 +1739,8 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
       ktab = item_time_slot(P, dyn, h, tid, P.inv_alpha);
     }
     TimeRun<A> run;                           // fast path: by float-exponent index
-    typename A::L *my_t = TIME ? tacc + h * P.time_hs + (lane & ((1 << P.time_cs) - 1)) : nullptr;
-    typename A::G *dp_item = POS ? (typename A::G *)P.dpos_part + si.start * P.H + h : nullptr;
+    typename A::L *my_t = TIME_T ? tacc + h * P.time_hs + (lane & ((1 << P.time_cs) - 1)) : nullptr;
+    typename A::G *dp_item = POS_T ? (typename A::G *)P.dpos_part + si.start * P.H + h : nullptr;
 
     // At d=128 (SPLIT) a wave's dK and dV accumulators together would take
     // 128 registers and hold the kernel to one wave per SIMD: there each
@@ -1591,8 +1763,8 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
       lds_barrier();
       qr.store(sm.t.a, tid);
       dr.store(sm.t.b, tid);
-      if constexpr (POS) {
-        pos_store<true>(pos_v, P.inv_alpha, sm.pos, tid);
+      if constexpr (POS) pos_store<true>(pos_v, P.inv_alpha, sm.pos, tid);
+      if constexpr (POS_T) {
         if (pend_p) atomicAdd(pend_p, pend_v);
         pend_p = nullptr;
         if (qt > q0 && tid < 2 * TILE - 1) {
@@ -1734,7 +1906,7 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
               dsv[e] = 0.0f;
             }
         }
-        if constexpr (POS) {
+        if constexpr (POS_T) {
           // element (i, j) -> slot i_loc - j_loc + 63, i_loc = ib + c_row(r, 0).
           // A register quad holds rows i0 .. i0+3 of the lane's key, so
           // element (i0 + k) of lane l+k lies on the diagonal of element i0
@@ -1764,7 +1936,7 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
             }
           }
         }
-        if (TIME) {
+        if (TIME_T) {
           // slow tiles accumulate by bucket straight into the work-group
           // histogram; fast tiles by float-exponent index, folded per item
           if (!slow) {
@@ -1829,12 +2001,12 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
     }
 
     // close the d_time runs; sum the two query halves, store dK, dV (bf16)
-    if (TIME) run.flush(my_t, P.nb, P.time_cs);
+    if (TIME_T) run.flush(my_t, P.nb, P.time_cs);
     lds_barrier();
     // one head's sums leave with the item (its next step's barriers order the
     // clearing); all heads' stay for the work-group's end
-    if (TIME && P.time_hs == 0) time_fold<DET>(P, tacc, tid, h, 1);
-    if constexpr (POS) {   // every diagonal of the last window is final
+    if (TIME_T && P.time_hs == 0) time_fold<DET>(P, tacc, tid, h, 1);
+    if constexpr (POS_T) {   // every diagonal of the last window is final
       if (tid < 2 * TILE - 1)
         dpos_retire<A>(smx.pwin[(phase - 1) & 1], smx.pwin[phase & 1], tid,
                        q1 - 1 - kt, true, si.len, dp_item, P.H, pend_p, pend_v);
@@ -1905,6 +2077,15 @@ __device__ __forceinline__ void dkv_kernel_fini(const KParams &P, typename TabAc
   }
 }
 
+template <int D, bool POS_T, bool TAB, bool DET>
+struct DqSmem {
+  StreamSmem<D> s;
+  typename TabAcc<DET>::L pwin[POS_T ? 2 : 1][2][2 * TILE];   // [window][g][slot]
+  // dO's second and third part (d = 128)
+  alignas(16) u16 mid[TAB && D == 128 ? TILE * D : 8];
+  alignas(16) u16 low[TAB && D == 128 ? TILE * D : 8];
+};
+
 // Backward, both item kinds in one launch over the combined list, whose
 // entries are dK/dV items (k-stationary) and dQ items (flagged,
 // q-stationary) in one longest-first order.
@@ -1933,7 +2114,10 @@ attn_bwd_kernel(KParams P) {
     const int h = item % P.H;
     if (e.tile & BWD_DQ_FLAG) {
       e.tile &= ~BWD_DQ_FLAG;
-      dq_item<D, POS, TIME, WIN>(P, sm, dyn, tid0, e, h, phase, nxt);
+      // (dO's parts lie where a dK/dV item holds V and its operands)
+      TabRefs<DET> tab{smx.vst, (u16 *)smx.xbuf, nullptr, tacc};
+      if constexpr (POS) tab.pwin = smx.pwin;
+      dq_item<D, POS, TIME, WIN, DET>(P, sm, tab, dyn, tid0, e, h, phase, nxt);
     } else {
       dkv_item<D, POS, TIME, DET, D == 64, WIN>(P, smx, dyn, tacc, tid0, e, h, phase, pend_p,
                                                 pend_v, nxt, P.fuse_dq0 ? dsb : nullptr);
@@ -1943,19 +2127,36 @@ attn_bwd_kernel(KParams P) {
 }
 
 // Backward, dQ: persistent work-groups pop q-tile items longest first.
-template <int D, bool POS, bool TIME, bool WIN>
-__global__ void __launch_bounds__(THREADS, D == 64 ? (TIME ? 2 : 3) : 2)
+template <int D, bool POS, bool TIME, bool WIN, bool DET>
+__global__ void __launch_bounds__(THREADS, D == 64 ? (TIME || (WIN && POS) ? 2 : 3) : 2)
 attn_bwd_dq_kernel(KParams P) {
-  __shared__ StreamSmem<D> sm;
-  extern __shared__ float dyn_q[];            // time tables
+  typedef TabAcc<DET> A;
+  constexpr bool TAB = WIN && (POS || TIME);
+  __shared__ DqSmem<D, WIN && POS, TAB, DET> smq;
+  StreamSmem<D> &sm = smq.s;
+  extern __shared__ double dyn_q[];           // (tables) time histogram, then time tables
+  typename A::L *hist = (typename A::L *)dyn_q;
+  float *dyn = (float *)(dyn_q + (TAB && TIME ? P.time_n : 0));
   const int tid0 = threadIdx.x;
   const int n_items = P.ctrl[CTRL_N_ENTRIES] * P.H;
+  if constexpr (TAB && TIME)
+    for (int x = tid0; x < P.time_n; x += THREADS) hist[x] = 0;
+  if constexpr (TAB && POS)
+    for (int x = tid0; x < 2 * 2 * 2 * TILE; x += THREADS) (&smq.pwin[0][0][0])[x] = 0;
   if (tid0 < 2) sm.flag[tid0] = 0;
   lds_barrier();
+  const TabRefs<DET> tab{smq.mid, smq.low, smq.pwin, hist};
   int phase = 0;
   int nxt = 0;
   for (int item = blockIdx.x; item < n_items; item = take_next(&sm.item, tid0, nxt))
-    dq_item<D, POS, TIME, WIN>(P, sm, dyn_q, tid0, P.list[item / P.H], item % P.H, phase, nxt);
+    dq_item<D, POS, TIME, WIN, DET>(P, sm, tab, dyn, tid0, P.list[item / P.H], item % P.H, phase,
+                                    nxt);
+  if constexpr (TAB && TIME) {
+    if (P.time_hs != 0) {
+      lds_barrier();
+      time_fold<DET>(P, hist, tid0, 0, P.H);
+    }
+  }
 }
 
 // Backward, dK/dV and the table gradients: persistent work-groups pop k-tile
@@ -2045,8 +2246,12 @@ constexpr int64_t LDS_BYTES = 160 * 1024;            // of a compute unit
 int64_t dkv128_room(const Problem &p) {
   static_assert(sizeof(DkvSmem<128, true, true>) == sizeof(DkvSmem<128, true, false>) &&
                 sizeof(DkvSmem<128, false, true>) == sizeof(DkvSmem<128, false, false>));
-  return LDS_BYTES / 2 - (int64_t)(p.has_pos ? sizeof(DkvSmem<128, true, false>)
-                                             : sizeof(DkvSmem<128, false, false>));
+  int64_t tiles = (int64_t)(p.has_pos ? sizeof(DkvSmem<128, true, false>)
+                                      : sizeof(DkvSmem<128, false, false>));
+  if (WINDOWED)        // the histogram is the dQ items'
+    tiles = std::max(tiles, (int64_t)(p.has_pos ? sizeof(DqSmem<128, true, true, false>)
+                                                : sizeof(DqSmem<128, false, true, false>)));
+  return LDS_BYTES / 2 - tiles;
 }
 // a slot of 128 buckets and two counters for each fit
 static_assert(LDS_BYTES / 2 - sizeof(DkvSmem<128, true, false>) >=
@@ -2055,14 +2260,13 @@ bool all_heads(const Problem &p, Pass pass) {
   const size_t budget = p.d != 64          ? ALL_HEADS_BUDGET / 4
                         : pass == Pass::FWD ? ALL_HEADS_BUDGET / 2
                                             : ALL_HEADS_BUDGET;
-  if (p.d != 64 && pass == Pass::DKV && p.H > 1) return false;
+  if (p.d != 64 && (pass == Pass::DKV || (WINDOWED && pass == Pass::DQ)) && p.H > 1) return false;
   return p.has_time && sizeof(float) * (size_t)p.H * (KTAB + p.nb) <= budget;
 }
 size_t slot_bytes(const Problem &p, bool all) {
   return p.has_time ? sizeof(float) * (size_t)(all ? p.H : 1) * (KTAB + p.nb) : 0;
 }
 size_t slots_bytes(const Problem &p, Pass pass) { return slot_bytes(p, all_heads(p, pass)); }
-size_t q_dyn_bytes(const Problem &p) { return slots_bytes(p, Pass::DQ); }
 size_t fwd_dyn_bytes(const Problem &p) { return slots_bytes(p, Pass::FWD); }
 // The dK/dV work-group's d_time histogram: every head's, folded once at the
 // work-group's end, where those take at most KEEP_BYTES (two or more counters a
@@ -2086,6 +2290,10 @@ TimeHist time_hist(const Problem &p) {
   t.hs = keep ? p.nb << t.cs : 0;
   t.n <<= t.cs;
   return t;
+}
+size_t q_dyn_bytes(const Problem &p) {
+  return slots_bytes(p, Pass::DQ) +
+         (WINDOWED && p.has_time ? sizeof(double) * (size_t)time_hist(p).n : 0);
 }
 size_t k_dyn_bytes(const Problem &p) {
   return p.has_time ? slots_bytes(p, Pass::DKV) + sizeof(double) * (size_t)time_hist(p).n : 0;
@@ -2123,6 +2331,7 @@ KParams make_params(const AttnArgs &a, int32_t *pop, const WorkEntry *list) {
   P.sinks = a.p.sinks;
   P.far_chunk = a.L.far_chunk;
   P.far_slots = (int32_t)a.L.far_entries;
+  P.o_full = a.o_full;
   P.far_part = a.L.far_chunk ? (float *)((char *)a.ws + a.L.far_part) : nullptr;
   return P;
 }
@@ -2143,26 +2352,47 @@ KParams make_params(const AttnArgs &a, int32_t *pop, const WorkEntry *list) {
   } while (0)
 
 template <int D, bool POS, bool TIME>
-constexpr auto attn_fwd_direct = attn_fwd_kernel<D, POS, TIME, 1, true, WINDOWED>;
+constexpr auto attn_fwd_direct = attn_fwd_kernel<D, POS, TIME, 1, true, WINDOWED, false>;
 
 template <int D, bool POS, bool TIME>
-constexpr auto attn_fwd_single = attn_fwd_kernel<D, POS, TIME, 1, false, WINDOWED>;
+constexpr auto attn_fwd_single = attn_fwd_kernel<D, POS, TIME, 1, false, WINDOWED, false>;
+
+// (windowed, with a table: o_full is written)
+template <int D, bool POS, bool TIME>
+constexpr auto attn_fwd_direct_x =
+    attn_fwd_kernel<D, POS, TIME, 1, true, WINDOWED, WINDOWED && (POS || TIME)>;
 
 template <int D, bool POS, bool TIME>
-constexpr auto attn_bwd_dq = attn_bwd_dq_kernel<D, POS, TIME, WINDOWED>;
+constexpr auto attn_fwd_single_x =
+    attn_fwd_kernel<D, POS, TIME, 1, false, WINDOWED, WINDOWED && (POS || TIME)>;
+
+// Table gradients are the dK/dV items' in the causal kernels, the dQ items' in the
+// windowed ones; the other kind has no deterministic form of its own.
+template <int D, bool POS, bool TIME, bool DET>
+constexpr auto attn_bwd_dq =
+    attn_bwd_dq_kernel<D, POS, TIME, WINDOWED, WINDOWED && DET && (POS || TIME)>;
 
 template <int D, bool POS, bool TIME, bool DET>
 constexpr auto attn_bwd_both = attn_bwd_kernel<D, POS, TIME, DET, WINDOWED>;
 
 template <int D, bool POS, bool TIME, bool DET>
-constexpr auto attn_bwd_dkv = attn_bwd_dkv_kernel<D, POS, TIME, DET, WINDOWED>;
+constexpr auto attn_bwd_dkv = attn_bwd_dkv_kernel<D, POS, TIME, DET && !WINDOWED, WINDOWED>;
+
+template <int D, bool POS, bool TIME>
+constexpr auto attn_bwd_far = attn_bwd_far_kernel<D, POS, TIME, false>;
 
 // The forward's items of two query tiles (d = 64 only, see fwd_pairs).
+template <bool X>
+auto attn_fwd_pair_of(const Problem &p) {
+  return p.has_pos ? (p.has_time ? attn_fwd_kernel<64, true, true, 2, false, WINDOWED, X>
+                                 : attn_fwd_kernel<64, true, false, 2, false, WINDOWED, X>)
+                   : (p.has_time ? attn_fwd_kernel<64, false, true, 2, false, WINDOWED, X>
+                                 : attn_fwd_kernel<64, false, false, 2, false, WINDOWED, false>);
+}
 auto attn_fwd_pair(const Problem &p) {
-  return p.has_pos ? (p.has_time ? attn_fwd_kernel<64, true, true, 2, false, WINDOWED>
-                                 : attn_fwd_kernel<64, true, false, 2, false, WINDOWED>)
-                   : (p.has_time ? attn_fwd_kernel<64, false, true, 2, false, WINDOWED>
-                                 : attn_fwd_kernel<64, false, false, 2, false, WINDOWED>);
+  if constexpr (WINDOWED)
+    if (p.exact) return attn_fwd_pair_of<true>(p);
+  return attn_fwd_pair_of<false>(p);
 }
 
 // As HSTU_DISPATCH, for the kernels that accumulate the table gradients
@@ -2209,8 +2439,12 @@ bool direct_fits(const Problem &p, int dev) {
   if (p.max_entries * p.H > 8 * (int64_t)device_info(dev).num_cu) return false;
   if (p.dtype != HSTU_BF16) return 2 * p.max_entries * p.H <= 2 * device_info(dev).num_cu;
   int grid = 0;
-  HSTU_DISPATCH(attn_fwd_direct, p.d, p.has_pos, p.has_time,
-                grid = persistent_grid(kfn, slot_bytes(p, false), p.max_entries * p.H, dev));
+  if (p.exact)
+    HSTU_DISPATCH(attn_fwd_direct_x, p.d, p.has_pos, p.has_time,
+                  grid = persistent_grid(kfn, slot_bytes(p, false), p.max_entries * p.H, dev));
+  else
+    HSTU_DISPATCH(attn_fwd_direct, p.d, p.has_pos, p.has_time,
+                  grid = persistent_grid(kfn, slot_bytes(p, false), p.max_entries * p.H, dev));
   return p.max_entries * p.H <= grid;
 }
 
@@ -2219,8 +2453,12 @@ int fwd_grid(const Problem &p, int dev) {
   if (fwd_pairs(p))
     return persistent_grid(attn_fwd_pair(p), fwd_dyn_bytes(p), items, dev, 2 * THREADS);
   int grid = 1;
-  HSTU_DISPATCH(attn_fwd_single, p.d, p.has_pos, p.has_time,
-                grid = persistent_grid(kfn, fwd_dyn_bytes(p), items, dev));
+  if (p.exact)
+    HSTU_DISPATCH(attn_fwd_single_x, p.d, p.has_pos, p.has_time,
+                  grid = persistent_grid(kfn, fwd_dyn_bytes(p), items, dev));
+  else
+    HSTU_DISPATCH(attn_fwd_single, p.d, p.has_pos, p.has_time,
+                  grid = persistent_grid(kfn, fwd_dyn_bytes(p), items, dev));
   return grid;
 }
 
@@ -2233,7 +2471,7 @@ int bwd_grid(const Problem &p, int dev) {
 
 int bwd_dq_grid(const Problem &p, int dev) {
   int grid = 1;
-  HSTU_DISPATCH(attn_bwd_dq, p.d, p.has_pos, p.has_time,
+  HSTU_DISPATCH_TAB(attn_bwd_dq, p.d, p.has_pos, p.has_time, p.deterministic,
                 grid = persistent_grid(kfn, q_dyn_bytes(p), p.max_entries * p.H, dev));
   return grid;
 }
@@ -2254,9 +2492,13 @@ hipError_t launch_fwd(const AttnArgs &a, void *o, bool direct, hipStream_t s) {
     P.off = a.off;
     P.T = p.T;
     P.B = p.B;
-    HSTU_DISPATCH(attn_fwd_direct, p.d, p.has_pos, p.has_time,
-                  hipLaunchKernelGGL(kfn, dim3((unsigned)(p.max_entries * p.H)), dim3(THREADS),
-                                     slot_bytes(p, false), s, P));
+    const dim3 grid((unsigned)(p.max_entries * p.H));
+    if (p.exact)
+      HSTU_DISPATCH(attn_fwd_direct_x, p.d, p.has_pos, p.has_time,
+                    hipLaunchKernelGGL(kfn, grid, dim3(THREADS), slot_bytes(p, false), s, P));
+    else
+      HSTU_DISPATCH(attn_fwd_direct, p.d, p.has_pos, p.has_time,
+                    hipLaunchKernelGGL(kfn, grid, dim3(THREADS), slot_bytes(p, false), s, P));
     return hipGetLastError();
   }
   const bool pairs = fwd_pairs(p);
@@ -2267,6 +2509,9 @@ hipError_t launch_fwd(const AttnArgs &a, void *o, bool direct, hipStream_t s) {
   const int grid = fwd_grid(p, current_dev());
   if (pairs)
     hipLaunchKernelGGL(attn_fwd_pair(p), dim3(grid), dim3(2 * THREADS), fwd_dyn_bytes(p), s, P);
+  else if (p.exact)
+    HSTU_DISPATCH(attn_fwd_single_x, p.d, p.has_pos, p.has_time,
+                  hipLaunchKernelGGL(kfn, dim3(grid), dim3(THREADS), fwd_dyn_bytes(p), s, P));
   else
     HSTU_DISPATCH(attn_fwd_single, p.d, p.has_pos, p.has_time,
                   hipLaunchKernelGGL(kfn, dim3(grid), dim3(THREADS), fwd_dyn_bytes(p), s, P));
@@ -2279,6 +2524,10 @@ hipError_t launch_bwd(const AttnArgs &a, const void *dO, void *dq, void *dk, voi
   const Problem &p = a.p;
   auto outputs = [&](KParams &P) {
     P.dO = (const u16 *)dO;
+    if (a.L.dO_mid) {
+      P.dO_mid = (const u16 *)(ws + a.L.dO_mid);
+      P.dO_low = (const u16 *)(ws + a.L.dO_low);
+    }
     P.out0 = (u16 *)dk;
     P.out1 = (u16 *)dv;
     P.dq_out = (u16 *)dq;
@@ -2294,12 +2543,10 @@ hipError_t launch_bwd(const AttnArgs &a, const void *dO, void *dq, void *dk, voi
       prof::Scope ps("attn_bwd_far", s);
       KParams P = make_params(a, nullptr, (const WorkEntry *)(ws + a.L.list_f));
       outputs(P);
-      P.dpos_part = a.L.dpos_part ? (void *)(ws + a.L.dpos_part) : nullptr;
-      P.dtime_part = a.L.dtime_part ? (void *)(ws + a.L.dtime_part) : nullptr;
       P.all_heads = all_heads(p, Pass::DKV) ? 1 : 0;
       const int64_t items = a.L.far_entries * ((p.sinks + TILE - 1) / TILE) * p.H;
-      HSTU_DISPATCH_TAB(attn_bwd_far_kernel, p.d, p.has_pos, p.has_time, p.deterministic,
-                        hipLaunchKernelGGL(kfn, dim3(persistent_grid(kfn, k_dyn_bytes(p), items,
+      HSTU_DISPATCH(attn_bwd_far, p.d, p.has_pos, p.has_time,
+                    hipLaunchKernelGGL(kfn, dim3(persistent_grid(kfn, k_dyn_bytes(p), items,
                                                                      current_dev())),
                                            dim3(THREADS), k_dyn_bytes(p), s, P));
       const hipError_t e = hipGetLastError();
@@ -2314,8 +2561,7 @@ hipError_t launch_bwd(const AttnArgs &a, const void *dO, void *dq, void *dk, voi
     P.dpos_part = a.L.dpos_part ? (void *)(ws + a.L.dpos_part) : nullptr;
     P.dtime_part = a.L.dtime_part ? (void *)(ws + a.L.dtime_part) : nullptr;
     P.all_heads = all_heads(p, Pass::DKV) ? 1 : 0;
-    // must match the scheduler's choice (sched_args)
-    P.fuse_dq0 = p.d == 64 ? 1 : 0;
+    P.fuse_dq0 = fuse_dq0(p) ? 1 : 0;
     HSTU_DISPATCH_TAB(attn_bwd_both, p.d, p.has_pos, p.has_time, p.deterministic,
                       hipLaunchKernelGGL(kfn, dim3(a.L.bwd_grid_both), dim3(THREADS),
                                          k_dyn_bytes(p), s, P));
@@ -2339,8 +2585,10 @@ hipError_t launch_bwd(const AttnArgs &a, const void *dO, void *dq, void *dk, voi
   KParams P = make_params(a, (int32_t *)(ws + a.L.ctrl) + CTRL_POP_DQ,
                           (const WorkEntry *)(ws + a.L.list_q));
   outputs(P);
+  P.dpos_part = a.L.dpos_part ? (void *)(ws + a.L.dpos_part) : nullptr;
+  P.dtime_part = a.L.dtime_part ? (void *)(ws + a.L.dtime_part) : nullptr;
   P.all_heads = all_heads(p, Pass::DQ) ? 1 : 0;
-  HSTU_DISPATCH(attn_bwd_dq, p.d, p.has_pos, p.has_time,
+  HSTU_DISPATCH_TAB(attn_bwd_dq, p.d, p.has_pos, p.has_time, p.deterministic,
                 hipLaunchKernelGGL(kfn, dim3(a.L.bwd_grid_dq), dim3(THREADS), q_dyn_bytes(p),
                                    s, P));
   return hipGetLastError();

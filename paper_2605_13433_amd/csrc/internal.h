@@ -90,12 +90,16 @@ struct Problem {
   // 0 .. N)
   bool windowed = false;
   int32_t window = 0, sinks = 0;
+  // windowed bf16 with a bias table, o kept in float32: the forward and backward
+  // carry A, o and dO as exactly as float32 does (attn_bf16_impl.h, "exact tables")
+  bool exact = false;
 };
 
 // Workspace carve-up; offsets in bytes from the workspace base, each region
 // 256-byte aligned.  Regions with size 0 are absent.
 struct Layout {
   size_t ctrl, seqinfo, list_q, list_k, list_b, list_p, dO, dpos_part, dtime_part, total;
+  size_t dO_mid, dO_low;              // the second and third part of dO (exact)
   // persistent grids of the bf16 backward kernels (combined, dQ, dK/dV) and
   // whether the combined one runs (small problems) or the other two
   int bwd_grid_both, bwd_grid_dq, bwd_grid_dkv;
@@ -200,7 +204,14 @@ struct AttnArgs {
   void *ws;
   Layout L;
   Problem p;
+  float *o_full = nullptr;
 };
+
+// Whether the combined backward's dK/dV items of first k-tiles compute their q-tile's dQ
+// (the scheduler then lists no such dQ items).
+inline bool fuse_dq0(const Problem &p) {
+  return p.d == 64 && !(p.windowed && (p.has_pos || p.has_time));
+}
 
 hipError_t launch_attn_fwd_bf16(const AttnArgs &a, void *o, bool direct, hipStream_t s);
 // dQ, dK, dV and the table-gradient partials: one combined launch, or a
@@ -237,13 +248,14 @@ hipError_t launch_window_fwd_f32(const AttnArgs &a, void *o, bool direct, hipStr
 hipError_t launch_window_bwd_f32(const AttnArgs &a, const void *dO, void *dq, void *dk, void *dv,
                                  float *d_pos, float *d_time, hipStream_t s);
 
-hipError_t launch_ln_fwd(const Problem &p, const void *o, const void *u,
+// (o_full: the same in float32, read instead where it is given, HSTU_BF16)
+hipError_t launch_ln_fwd(const Problem &p, const void *o, const float *o_full, const void *u,
                          void *y, float *mean, float *rstd, hipStream_t s);
 // LayerNorm backward with the scheduler's work-group appended: builds the
 // backward's lists (as launch_schedule) in the same launch.
 hipError_t launch_ln_bwd_sched(const Problem &p, const void *dy, const void *u,
-                               const void *o, const float *mean, const float *rstd,
-                               void *du, void *dO, void *dpos_part,
+                               const void *o, const float *o_full, const float *mean,
+                               const float *rstd, void *du, void *dO, void *dpos_part,
                                const int64_t *seq_offsets, void *ws, const Layout &L,
                                const GradOut *go, hipStream_t s);
 hipError_t launch_finalize_tables(const AttnArgs &a, float *d_pos,

@@ -13,6 +13,9 @@
 // statistics are shuffle sums over the token's lane group.  Otherwise one
 // wave64 walks a token in 512-wide chunks.  These kernels are HBM-bound
 // (each feature is read and written once or twice).
+//
+// The windowed bf16 operator with a bias table (attn_bf16_impl.h, "exact tables")
+// reads o in float32 (TO) and writes dO as three bf16 parts (PARTS).
 #include <algorithm>
 
 #include "internal.h"
@@ -69,6 +72,25 @@ struct Vec8<float> {
   }
 };
 
+// f as a sum of three bf16 rows: the rounded values, and twice what is left.
+__device__ __forceinline__ void store_parts(u16 *a, u16 *b, u16 *c, const float (&f)[8]) {
+  u16 *to[3] = {a, b, c};
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = f[e];
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pack2(r[2 * e], r[2 * e + 1]);
+      r[2 * e] -= __uint_as_float(w[e] << 16);
+      r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+    }
+    *(uint4 *)to[p] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
 // Sum over the aligned group of L lanes (L a power of two) holding one token.
 template <int L>
 __device__ __forceinline__ float group_sum(float x) {
@@ -78,9 +100,9 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 // Fast path: F = 8 L, L = 64 / TPW lanes per token, TPW tokens per wave.
-template <typename T, int L>
+template <typename T, int L, typename TO = T>
 __global__ void __launch_bounds__(LN_THREADS)
-ln_fwd_group_kernel(const T *__restrict__ o, const T *__restrict__ u,
+ln_fwd_group_kernel(const TO *__restrict__ o, const T *__restrict__ u,
                     T *__restrict__ y, float *__restrict__ mean_out,
                     float *__restrict__ rstd_out, int64_t T_tokens) {
   constexpr int F = 8 * L, TPW = 64 / L;
@@ -89,7 +111,7 @@ ln_fwd_group_kernel(const T *__restrict__ o, const T *__restrict__ u,
   if (r >= T_tokens) return;
   const int64_t at = r * F + 8 * sub;
   float z[8], uu[8];
-  Vec8<T>::load(o + at, z);
+  Vec8<TO>::load(o + at, z);
   Vec8<T>::load(u + at, uu);
   float sum = 0.0f;
 #pragma unroll
@@ -118,12 +140,13 @@ __device__ __forceinline__ void silu_back8(const T *__restrict__ h, float g[8]) 
   for (int e = 0; e < 8; ++e) g[e] *= dsilu_f(hh[e]);
 }
 
-template <typename T, int L>
+template <typename T, int L, typename TO, bool PARTS>
 __device__ __forceinline__ void ln_bwd_group(const T *__restrict__ dy, const T *__restrict__ u,
-                                             const T *__restrict__ o,
+                                             const TO *__restrict__ o,
                                              const float *__restrict__ mean,
                                              const float *__restrict__ rstd,
                                              T *__restrict__ du, T *__restrict__ dO,
+                                             T *__restrict__ dO_mid, T *__restrict__ dO_low,
                                              uint64_t *__restrict__ dpos_part, int H,
                                              int64_t T_tokens, int block, int64_t du_stride,
                                              const T *__restrict__ du_h) {
@@ -133,7 +156,7 @@ __device__ __forceinline__ void ln_bwd_group(const T *__restrict__ dy, const T *
   if (r >= T_tokens) return;
   const int64_t at = r * F + 8 * sub;
   float z[8], g[8], uu[8];
-  Vec8<T>::load(o + at, z);
+  Vec8<TO>::load(o + at, z);
   Vec8<T>::load(dy + at, g);
   Vec8<T>::load(u + at, uu);
   const float mu = mean[r], rs = rstd[r];
@@ -157,25 +180,26 @@ __device__ __forceinline__ void ln_bwd_group(const T *__restrict__ dy, const T *
   const int64_t du_at = r * du_stride + 8 * sub;
   if (du_h) silu_back8(du_h + du_at, o_du);
   Vec8<T>::store(du + du_at, o_du);
-  Vec8<T>::store(dO + at, o_do);
+  if constexpr (PARTS) store_parts(dO + at, dO_mid + at, dO_low + at, o_do);
+  else Vec8<T>::store(dO + at, o_do);
   // the attention backward accumulates this token's d_pos partials (8
   // bytes each: a float, or 64-bit fixed point in the deterministic mode)
   if (dpos_part && sub < H) dpos_part[r * H + sub] = 0;
 }
 
-template <typename T>
+template <typename T, typename TO = T>
 __global__ void __launch_bounds__(LN_THREADS)
-ln_fwd_kernel(const T *__restrict__ o, const T *__restrict__ u,
+ln_fwd_kernel(const TO *__restrict__ o, const T *__restrict__ u,
               T *__restrict__ y, float *__restrict__ mean_out,
               float *__restrict__ rstd_out, int64_t T_tokens, int F) {
   const int lane = threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * LN_WAVES + (threadIdx.x >> 6);
   if (r >= T_tokens) return;
-  const T *orow = o + r * F;
+  const TO *orow = o + r * F;
   float sum = 0.0f;
   for (int f0 = lane * 8; f0 < F; f0 += 512) {
     float z[8];
-    Vec8<T>::load(orow + f0, z);
+    Vec8<TO>::load(orow + f0, z);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += z[e];
   }
@@ -183,14 +207,14 @@ ln_fwd_kernel(const T *__restrict__ o, const T *__restrict__ u,
   float sq = 0.0f;
   for (int f0 = lane * 8; f0 < F; f0 += 512) {
     float z[8];
-    Vec8<T>::load(orow + f0, z);
+    Vec8<TO>::load(orow + f0, z);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sq += (z[e] - mu) * (z[e] - mu);
   }
   const float rstd = rsqrtf(wave_sum(sq) / (float)F + HSTU_LN_EPS);
   for (int f0 = lane * 8; f0 < F; f0 += 512) {
     float z[8], uu[8], out[8];
-    Vec8<T>::load(orow + f0, z);
+    Vec8<TO>::load(orow + f0, z);
     Vec8<T>::load(u + r * F + f0, uu);
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = (z[e] - mu) * rstd * uu[e];
@@ -205,14 +229,14 @@ ln_fwd_kernel(const T *__restrict__ o, const T *__restrict__ u,
 // With `sched` set, the launch's first work-group (dispatched first, so its
 // serial phases overlap the rest) builds the backward's work lists
 // (sched_impl.h) while the others normalise.
-template <typename T>
+template <typename T, typename TO = T, bool PARTS = false>
 __global__ void __launch_bounds__(LN_THREADS)
 ln_bwd_kernel(const T *__restrict__ dy, const T *__restrict__ u,
-              const T *__restrict__ o, const float *__restrict__ mean,
+              const TO *__restrict__ o, const float *__restrict__ mean,
               const float *__restrict__ rstd, T *__restrict__ du,
               T *__restrict__ dO, uint64_t *__restrict__ dpos_part, int H,
               int64_t T_tokens, int F, SchedArgs sa, int sched, int64_t du_stride,
-              const T *__restrict__ du_h) {
+              const T *__restrict__ du_h, T *__restrict__ dO_mid, T *__restrict__ dO_low) {
   if (sched && blockIdx.x == 0) {
     __shared__ SchedSmem ssm;
     build_schedule<LN_THREADS>(sa, ssm, threadIdx.x);
@@ -222,8 +246,9 @@ ln_bwd_kernel(const T *__restrict__ dy, const T *__restrict__ u,
   switch (F) {
 #define HSTU_LN_GROUP(LL)                                                               \
   case 8 * LL:                                                                          \
-    ln_bwd_group<T, LL>(dy, u, o, mean, rstd, du, dO, dpos_part, H, T_tokens,            \
-                        (int)blockIdx.x - sched, du_stride, du_h);                      \
+    ln_bwd_group<T, LL, TO, PARTS>(dy, u, o, mean, rstd, du, dO, dO_mid, dO_low,         \
+                                   dpos_part, H, T_tokens, (int)blockIdx.x - sched,     \
+                                   du_stride, du_h);                                    \
     return;
     HSTU_LN_GROUP(1) HSTU_LN_GROUP(2) HSTU_LN_GROUP(4) HSTU_LN_GROUP(8)
     HSTU_LN_GROUP(16) HSTU_LN_GROUP(32) HSTU_LN_GROUP(64)
@@ -239,7 +264,7 @@ ln_bwd_kernel(const T *__restrict__ dy, const T *__restrict__ u,
   float sg = 0.0f, sgn = 0.0f;
   for (int f0 = lane * 8; f0 < F; f0 += 512) {
     float z[8], g[8], uu[8];
-    Vec8<T>::load(o + base + f0, z);
+    Vec8<TO>::load(o + base + f0, z);
     Vec8<T>::load(dy + base + f0, g);
     Vec8<T>::load(u + base + f0, uu);
 #pragma unroll
@@ -254,7 +279,7 @@ ln_bwd_kernel(const T *__restrict__ dy, const T *__restrict__ u,
   const float mgn = wave_sum(sgn) / (float)F;
   for (int f0 = lane * 8; f0 < F; f0 += 512) {
     float z[8], g[8], uu[8], o_du[8], o_do[8];
-    Vec8<T>::load(o + base + f0, z);
+    Vec8<TO>::load(o + base + f0, z);
     Vec8<T>::load(dy + base + f0, g);
     Vec8<T>::load(u + base + f0, uu);
 #pragma unroll
@@ -265,7 +290,10 @@ ln_bwd_kernel(const T *__restrict__ dy, const T *__restrict__ u,
     }
     if (du_h) silu_back8(du_h + r * du_stride + f0, o_du);
     Vec8<T>::store(du + r * du_stride + f0, o_du);
-    Vec8<T>::store(dO + base + f0, o_do);
+    if constexpr (PARTS)
+      store_parts(dO + base + f0, dO_mid + base + f0, dO_low + base + f0, o_do);
+    else
+      Vec8<T>::store(dO + base + f0, o_do);
   }
   // the attention backward accumulates this token's d_pos partials
   if (dpos_part && lane < H) dpos_part[r * H + lane] = 0;
@@ -379,15 +407,15 @@ static unsigned ln_blocks(int64_t T, int tpw) {
   return (unsigned)((T + per - 1) / per);
 }
 
-template <typename T>
-hipError_t launch_ln_fwd_t(const Problem &p, const T *o, const T *u, T *y, float *mean,
+template <typename T, typename TO>
+hipError_t launch_ln_fwd_t(const Problem &p, const TO *o, const T *u, T *y, float *mean,
                            float *rstd, hipStream_t s) {
   const int F = p.H * p.d;
   const int L = ln_group_lanes(F);
   switch (L) {
 #define HSTU_LN_GROUP(LL)                                                               \
   case LL:                                                                              \
-    hipLaunchKernelGGL((ln_fwd_group_kernel<T, LL>), dim3(ln_blocks(p.T, 64 / LL)),      \
+    hipLaunchKernelGGL((ln_fwd_group_kernel<T, LL, TO>), dim3(ln_blocks(p.T, 64 / LL)),  \
                        dim3(LN_THREADS), 0, s, o, u, y, mean, rstd, p.T);               \
     return hipGetLastError();
     HSTU_LN_GROUP(1) HSTU_LN_GROUP(2) HSTU_LN_GROUP(4) HSTU_LN_GROUP(8)
@@ -396,13 +424,15 @@ hipError_t launch_ln_fwd_t(const Problem &p, const T *o, const T *u, T *y, float
     default:
       break;
   }
-  hipLaunchKernelGGL(ln_fwd_kernel<T>, dim3(ln_blocks(p.T, 1)), dim3(LN_THREADS), 0, s, o, u,
-                     y, mean, rstd, p.T, F);
+  hipLaunchKernelGGL((ln_fwd_kernel<T, TO>), dim3(ln_blocks(p.T, 1)), dim3(LN_THREADS), 0, s, o,
+                     u, y, mean, rstd, p.T, F);
   return hipGetLastError();
 }
 
-hipError_t launch_ln_fwd(const Problem &p, const void *o, const void *u,
+hipError_t launch_ln_fwd(const Problem &p, const void *o, const float *o_full, const void *u,
                          void *y, float *mean, float *rstd, hipStream_t s) {
+  if (p.dtype == HSTU_BF16 && o_full)
+    return launch_ln_fwd_t<u16>(p, o_full, (const u16 *)u, (u16 *)y, mean, rstd, s);
   if (p.dtype == HSTU_BF16)
     return launch_ln_fwd_t<u16>(p, (const u16 *)o, (const u16 *)u, (u16 *)y, mean, rstd, s);
   return launch_ln_fwd_t<float>(p, (const float *)o, (const float *)u, (float *)y, mean, rstd,
@@ -410,8 +440,8 @@ hipError_t launch_ln_fwd(const Problem &p, const void *o, const void *u,
 }
 
 hipError_t launch_ln_bwd_sched(const Problem &p, const void *dy, const void *u,
-                               const void *o, const float *mean, const float *rstd,
-                               void *du, void *dO, void *dpos_part_v,
+                               const void *o, const float *o_full, const float *mean,
+                               const float *rstd, void *du, void *dO, void *dpos_part_v,
                                const int64_t *seq_offsets, void *ws, const Layout &L,
                                const GradOut *go, hipStream_t s) {
   uint64_t *dpos_part = (uint64_t *)dpos_part_v;
@@ -419,16 +449,23 @@ hipError_t launch_ln_bwd_sched(const Problem &p, const void *dy, const void *u,
   const SchedArgs sa = sched_args(seq_offsets, p, ws, L);
   const int GL = ln_group_lanes(F);
   const dim3 grid(ln_blocks(p.T, GL ? 64 / GL : 1) + 1);
-  if (p.dtype == HSTU_BF16)
+  if (p.dtype == HSTU_BF16 && L.dO_mid)
+    hipLaunchKernelGGL((ln_bwd_kernel<u16, float, true>), grid, dim3(LN_THREADS), 0, s,
+                       (const u16 *)dy, (const u16 *)u, o_full, mean, rstd, (u16 *)du, (u16 *)dO,
+                       dpos_part, p.H, p.T, F, sa, 1, go ? go->stride : (int64_t)F,
+                       go ? (const u16 *)go->h_du : nullptr, (u16 *)((char *)ws + L.dO_mid),
+                       (u16 *)((char *)ws + L.dO_low));
+  else if (p.dtype == HSTU_BF16)
     hipLaunchKernelGGL(ln_bwd_kernel<u16>, grid, dim3(LN_THREADS), 0, s,
                        (const u16 *)dy, (const u16 *)u, (const u16 *)o, mean, rstd,
                        (u16 *)du, (u16 *)dO, dpos_part, p.H, p.T, F, sa, 1,
-                       go ? go->stride : (int64_t)F, go ? (const u16 *)go->h_du : nullptr);
+                       go ? go->stride : (int64_t)F, go ? (const u16 *)go->h_du : nullptr,
+                       (u16 *)nullptr, (u16 *)nullptr);
   else
     hipLaunchKernelGGL(ln_bwd_kernel<float>, grid, dim3(LN_THREADS), 0, s,
                        (const float *)dy, (const float *)u, (const float *)o, mean, rstd,
                        (float *)du, (float *)dO, dpos_part, p.H, p.T, F, sa, 1, (int64_t)F,
-                       (const float *)nullptr);
+                       (const float *)nullptr, (float *)nullptr, (float *)nullptr);
   return hipGetLastError();
 }
 

@@ -363,7 +363,7 @@ inline SchedArgs sched_args(const int64_t *seq_offsets, const Problem &p, void *
   a.cap_p = (int32_t)pair_entries(p);
   a.H = p.H;
   a.grid_hint = 4 * L.num_cu;
-  a.fuse_dq0 = L.list_b && L.bwd_combined && p.d == 64 ? 1 : 0;
+  a.fuse_dq0 = L.list_b && L.bwd_combined && fuse_dq0(p) ? 1 : 0;
   a.check = p.check_offsets ? 1 : 0;
   a.zero_out = L.dtime_part ? (float *)(base + L.dtime_part) : nullptr;
   // 8 bytes per partial entry (see make_layout): DTIME_BINS histograms for

@@ -45,7 +45,8 @@ class Rab(ctypes.Structure):
 
 
 class Window(ctypes.Structure):
-    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("o_full", ctypes.c_void_p)]
 
 
 class FwdOut(ctypes.Structure):
@@ -237,13 +238,13 @@ def hstu_jagged_attn_bwd(q, k, v, u, seq_offsets, B, max_len, H, d,
         ctypes.byref(io), _stream(stream)))
 
 
-def make_window(window, sinks=0) -> Optional[Window]:
+def make_window(window, sinks=0, o_full=None) -> Optional[Window]:
     """None without a window (the plain operator)."""
     if window is None:
         if sinks:
             raise ValueError("sinks are given without a window")
         return None
-    return Window(int(window), int(sinks))
+    return Window(int(window), int(sinks), _ptr(o_full))
 
 
 def hstu_jagged_window_attn_workspace_bytes(B, max_len, H, d, total_tokens, for_bwd, dtype_code,
@@ -429,7 +430,11 @@ class Plan:
         self.B = seq_offsets.numel() - 1
         self.N, self.H, self.d, self.T = int(max_len), H, d, T
         self.rab = make_rab(pos_w, time_w, timestamps, num_buckets, alpha)
-        self.win = make_window(window, sinks)
+        # what the windowed bf16 backward needs for the tables' gradients
+        self.o_full = (torch.empty(T, H, d, dtype=torch.float32, device=dev)
+                       if window is not None and backward and q.dtype == torch.bfloat16 and
+                       (pos_w is not None or time_w is not None) else None)
+        self.win = make_window(window, sinks, self.o_full)
         self._keep = (pos_w, time_w, timestamps)
         code = _dtype_code(q)
         self.fwd_ws = _workspace(self._workspace_bytes(0, code), dev)

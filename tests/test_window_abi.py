@@ -53,6 +53,16 @@ def test_the_plain_checks_hold():
     assert "d_pos_w" in hstu.last_error()
 
 
+def test_the_tables_need_o():
+    io = hstu.BwdIO(hstu.HSTU_BF16, 10, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None,
+                    FAKE, 1 << 40)
+    rab = hstu.Rab(FAKE, None, None, 0)
+    rc = hstu.load_library().hstu_jagged_window_attn_bwd(
+        FAKE, FAKE, FAKE, FAKE, FAKE, 2, 64, 2, 64, ctypes.byref(rab), _win(4, 0),
+        ctypes.byref(io), None)
+    assert rc == -1 and "o_full" in hstu.last_error()
+
+
 def test_empty_batches():
     assert _fwd(_win(0, 0), T=0) == 0
     assert _bwd(_win(0, 0), T=0) == 0
