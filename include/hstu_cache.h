@@ -86,8 +86,8 @@ int hstu_cache_extend(const hstu_cache *c, const int32_t *slot_ids,
 /* Writes one layer's rows: rows row_offsets[r] .. row_offsets[r+1]-1 of k and v
  * ([total_rows][H][d]) become the tokens from start[r] on of sequence slot_ids[r]
  * (start as extend returned it; rows with start[r] < 0 are skipped).  row_offsets
- * (int64, n + 1) as seq_offsets in hstu_jagged.h; no row holds more than max_new
- * tokens.  With timestamps ([total_rows], and c->ts) those are written too: once a
+ * (int64, n + 1) as seq_offsets in hstu_jagged.h; of a row that holds more than
+ * max_new tokens the first max_new are written.  With timestamps ([total_rows], and c->ts) those are written too: once a
  * step, with any of its layers.  No two rows name the same tokens. */
 int hstu_cache_write(const hstu_cache *c, int32_t layer, const void *k,
                      const void *v, const int64_t *timestamps,

@@ -294,13 +294,44 @@ __device__ __forceinline__ bool pair_active(const KParams &P, int qt, int kt) {
   return kt <= qt && ((qt - kt) * TILE - (TILE - 1) < P.window || kt * TILE < P.sinks);
 }
 
-// Whether query row i_loc of tile qt does not see key row j_loc of tile kt.
+// The pairs of an edge tile that are not seen, for a lane that holds one query row and
+// keys j0 + c (rows of their tiles), or one key row and queries i0 + c.  The three
+// bounds are made opaque where they are used: the compiler would otherwise keep the
+// comparisons of every c in registers across the loop over tiles (36 of them, a
+// work-group less on a compute unit).  Without WIN (the diagonal tile) the causal rule.
 template <bool WIN>
-__device__ __forceinline__ bool hidden(const KParams &P, int qt, int kt, int i_loc, int j_loc) {
-  if constexpr (!WIN) return j_loc > i_loc;               // (the diagonal tile)
-  const int gap = i_loc - j_loc + (qt - kt) * TILE;
-  return gap < 0 || (gap >= P.window && j_loc >= P.sinks - kt * TILE);
-}
+struct HiddenKeys {
+  int causal, old, sink;
+  __device__ __forceinline__ HiddenKeys(const KParams &P, int qt, int kt, int i_loc, int j0)
+      : causal(i_loc), old(j0), sink(0) {
+    if constexpr (WIN) {
+      causal = i_loc - j0 + (qt - kt) * TILE;
+      old = causal - P.window;
+      sink = P.sinks - kt * TILE - j0;
+      asm volatile("" : "+v"(causal), "+v"(old), "+v"(sink));
+    }
+  }
+  __device__ __forceinline__ bool operator()(int c) const {
+    if constexpr (!WIN) return old + c > causal;
+    return c > causal || (c <= old && c >= sink);
+  }
+};
+template <bool WIN>
+struct HiddenQueries {
+  int causal, old;
+  __device__ __forceinline__ HiddenQueries(const KParams &P, int qt, int kt, int i0, int j_loc)
+      : causal(j_loc), old(i0) {
+    if constexpr (WIN) {
+      causal = j_loc - i0 - (qt - kt) * TILE;
+      old = j_loc < P.sinks - kt * TILE ? 2 * TILE : causal + P.window;
+      asm volatile("" : "+v"(causal), "+v"(old));
+    }
+  }
+  __device__ __forceinline__ bool operator()(int c) const {
+    if constexpr (!WIN) return old + c < causal;
+    return c < causal || c >= old;
+  }
+};
 
 // Last query tile of key tile kt that the windows of its keys reach.
 template <bool WIN>
@@ -849,7 +880,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, 
 // slice and timestamps, so no item starts with an exposed memory latency.
 // DIRECT: one item per work-group, found from the offsets (fwd_direct).
 template <int D, bool POS, bool TIME, int QT, bool DIRECT, bool WIN, bool EXACT>
-__global__ void __launch_bounds__(THREADS * QT, QT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(THREADS * QT, QT == 1 ? 2 : WIN ? 4 : 1)
 attn_fwd_kernel(KParams P) {
   static_assert(QT == 1 || !DIRECT, "direct items are one query tile");
   constexpr int NT = THREADS * QT, NW = 4 * QT;
@@ -1094,9 +1125,10 @@ attn_fwd_kernel(KParams P) {
         // the only one that can hold rows past the sequence, zero rows that
         // the same mask removes)
         if (edge) {
+          const HiddenKeys<WIN> hide(P, qt, kt, i_loc, kb);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (hidden<WIN>(P, qt, kt, i_loc, kb + c_row(8 * hh + e, 0))) av[e] = 0.0f;
+            if (hide(c_row(8 * hh + e, 0))) av[e] = 0.0f;
         }
         if constexpr (EXACT) {
           bf16x8 pa[3];
@@ -1492,9 +1524,10 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
         for (int e = 0; e < 8; ++e)
           dsv[e] = dq_ds(sg[e], da[8 * hh + e], x[e], P.alpha);
         if (pair_edge<WIN>(P, qt, kt)) {
+          const HiddenKeys<WIN> hide(P, qt, kt, i_loc, kb);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (hidden<WIN>(P, qt, kt, i_loc, kb + c_row(8 * hh + e, 0))) dsv[e] = 0.0f;
+            if (hide(c_row(8 * hh + e, 0))) dsv[e] = 0.0f;
         }
         if constexpr (TAB && POS) {
           // as the dK/dV item's (see there): element (i, j) -> slot i_loc - j_loc + 63,
@@ -1899,9 +1932,10 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
           // a real branch: selected without it, the mask's compares and
           // selects would run on every step
           asm volatile("");
+          const HiddenQueries<WIN> hide(P, qt, kt, ib, j_loc);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (hidden<WIN>(P, qt, kt, ib + c_row(8 * hh + e, 0), j_loc)) {
+            if (hide(c_row(8 * hh + e, 0))) {
               av[e] = 0.0f;
               dsv[e] = 0.0f;
             }

@@ -41,24 +41,32 @@ struct CollectSmem {
   int32_t at[ROUND * PLAN_WAVES + 1];
 };
 
-// Writes the pages p of [from, to) whose count is zero (ZERO) or not to out[0 ..], in
-// order, until `most` of them are found; returns their number.  All threads.
-template <bool ZERO>
-__device__ int32_t collect(const int32_t *refs, int32_t from, int32_t to, int32_t *out,
-                           int32_t most, CollectSmem &sm, int tid) {
+// The counts of pages p0 + k PLAN_THREADS + tid (past the pool none is read).
+__device__ __forceinline__ void load_counts(const int32_t *refs, int64_t p0, int32_t pages,
+                                            int tid, int32_t (&c)[ROUND]) {
+#pragma unroll
+  for (int k = 0; k < ROUND; ++k) {
+    const int64_t p = p0 + k * PLAN_THREADS + tid;
+    c[k] = p < pages ? refs[p] : 0;
+  }
+}
+
+// Writes the pages p that `want(p, count)` names to out[0 ..], in order, until `most` of
+// them are found; returns their number.  `c` holds the first round's counts.  All
+// threads.
+template <typename Want>
+__device__ __forceinline__ int32_t collect(const int32_t *refs, int32_t pages, int32_t *out,
+                                           int32_t most, CollectSmem &sm, int tid,
+                                           int32_t (&c)[ROUND], Want want) {
   const int lane = tid & 63, wv = tid >> 6;
   int32_t got = 0;
-  for (int64_t p0 = from; p0 < to && got < most; p0 += ROUND * PLAN_THREADS) {
-    int32_t c[ROUND];
-#pragma unroll
-    for (int k = 0; k < ROUND; ++k) {
-      const int64_t p = p0 + k * PLAN_THREADS + tid;
-      c[k] = p < to ? refs[p] : (ZERO ? 1 : 0);
-    }
+  for (int64_t p0 = 0; p0 < pages && got < most; p0 += ROUND * PLAN_THREADS) {
+    if (p0 > 0) load_counts(refs, p0, pages, tid, c);
     uint64_t hit[ROUND];
 #pragma unroll
     for (int k = 0; k < ROUND; ++k) {
-      hit[k] = __ballot(ZERO ? c[k] == 0 : c[k] != 0);
+      const int64_t p = p0 + k * PLAN_THREADS + tid;
+      hit[k] = __ballot(p < pages && want((int32_t)p, c[k]));
       if (lane == 0) sm.at[k * PLAN_WAVES + wv] = __popcll(hit[k]);
     }
     __syncthreads();
@@ -89,6 +97,9 @@ __device__ int32_t collect(const int32_t *refs, int32_t from, int32_t to, int32_
   return got < most ? got : most;
 }
 
+// Keeps the loads above it from being sunk to their use (emits nothing).
+__device__ __forceinline__ void issue_fence() { asm volatile("" ::: "memory"); }
+
 // Copies `bytes` (a multiple of 16) from src to dst, threads tid of nt.
 __device__ __forceinline__ void copy16(const char *src, char *dst, int64_t bytes, int tid, int nt) {
   const int64_t n = bytes >> 4;
@@ -96,6 +107,7 @@ __device__ __forceinline__ void copy16(const char *src, char *dst, int64_t bytes
   for (; x + 3 * nt < n; x += 4 * nt) {
     const uint4 a = ((const uint4 *)src)[x], b = ((const uint4 *)src)[x + nt],
                 c = ((const uint4 *)src)[x + 2 * nt], d = ((const uint4 *)src)[x + 3 * nt];
+    issue_fence();
     ((uint4 *)dst)[x] = a;
     ((uint4 *)dst)[x + nt] = b;
     ((uint4 *)dst)[x + 2 * nt] = c;
@@ -118,108 +130,153 @@ __global__ void cache_clear_kernel(CacheDev c) {
 }
 
 // -------------------------------------------------------------------- extend
-// A row's plan: pages it needs, the first of them in `fresh`, the shared page that is
-// copied (-1: none); `need` < 0: refused.
+// A row's plan: pages it needs, the first of them in the list of free pages, the shared
+// page that is copied (-1: none); `need` < 0: refused.
 struct RowPlan {
-  int32_t need, base, shared, reserved;
+  int32_t need, base, shared, len;
 };
 // A copy that the second launch makes: `rows` tokens of page src into page dst.
 struct PageCopy {
   int32_t src, dst, rows;
 };
 
+// LDS room of the plan: owners of the slots, free pages (both in the workspace where
+// there are more), and rows that need more pages than a thread writes by itself.
+constexpr int OWNERS_LDS = 8192, FRESH_LDS = 4096, PAGES_ALONE = 4;
+
+// One row: what it needs.  `owner` holds the first row that names each slot.
+__device__ __forceinline__ RowPlan plan_row(const CacheDev &c, int32_t r, int32_t s, int32_t cnt,
+                                            const int32_t *owner, int &bad) {
+  RowPlan p{-1, 0, -1, 0};
+  if (s < 0 || s >= c.slots) {
+    bad |= HSTU_CACHE_BAD_SLOT;
+    return p;
+  }
+  if (__hip_atomic_load(&owner[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != r) {
+    bad |= HSTU_CACHE_TWICE;
+    return p;
+  }
+  if (cnt < 0) {
+    bad |= HSTU_CACHE_BAD_COUNT;
+    return p;
+  }
+  p.len = slot_len(c.lens, c.slots, c.capacity, s);
+  if (cnt > c.capacity - p.len) {
+    bad |= HSTU_CACHE_FULL;
+    return p;
+  }
+  const int32_t had = pages_of(p.len, c.log_page);
+  p.need = pages_of((int64_t)p.len + cnt, c.log_page) - had;
+  if (cnt > 0 && (p.len & ((1 << c.log_page) - 1)) != 0) {
+    const int32_t last = c.tables[(int64_t)s * c.max_pages + had - 1];
+    if (last >= 0 && last < c.num_pages && c.refs[last] > 1) {
+      p.shared = last;
+      ++p.need;
+    }
+  }
+  return p;
+}
+
+// The chain of steps bounds it: the counts of the first 16384 pages are loaded before
+// anything else, owners and free pages lie in LDS, a thread keeps its row in registers
+// and writes up to PAGES_ALONE pages of it, the rest a wave a row.  (With all of this in
+// device memory and a wave a row: 32 rows of one token 15.7 us, 64 prompts 16.5.)
 __global__ void __launch_bounds__(PLAN_THREADS)
 cache_extend_kernel(CacheDev c, const int32_t *slot_ids, const int32_t *counts, int32_t n,
-                    int32_t *start, int32_t *owner, RowPlan *plan, int32_t *fresh,
+                    int32_t *start, int32_t *owner_ws, RowPlan *plan, int32_t *fresh_ws,
                     PageCopy *copies) {
   __shared__ int32_t sums[PLAN_WAVES];
   __shared__ CollectSmem cs;
+  __shared__ int32_t owner_lds[OWNERS_LDS], fresh_lds[FRESH_LDS];
+  __shared__ int32_t wide[PLAN_THREADS], n_wide;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  // the first row that names a slot owns it
+  int32_t refs0[ROUND];
+  load_counts(c.refs, 0, c.num_pages, tid, refs0);
+  const int32_t s0 = tid < n ? slot_ids[tid] : -1, cnt0 = tid < n ? counts[tid] : 0;
+  int32_t *owner = c.slots <= OWNERS_LDS ? owner_lds : owner_ws;
+  if (tid == 0) n_wide = 0;
   for (int r = tid; r < n; r += PLAN_THREADS) {
-    const int32_t s = slot_ids[r];
+    const int32_t s = r < PLAN_THREADS ? s0 : slot_ids[r];
     if (s >= 0 && s < c.slots) atomicExch(&owner[s], n);
   }
-  __threadfence();
+  if (owner == owner_ws) __threadfence();
   __syncthreads();
   for (int r = tid; r < n; r += PLAN_THREADS) {
-    const int32_t s = slot_ids[r];
+    const int32_t s = r < PLAN_THREADS ? s0 : slot_ids[r];
     if (s >= 0 && s < c.slots) atomicMin(&owner[s], r);
   }
-  __threadfence();
+  if (owner == owner_ws) __threadfence();
   __syncthreads();
 
   int64_t run = 0;
   int bad = 0;
+  RowPlan mine{-1, 0, -1, 0};                 // this thread's first row
   for (int r0 = 0; r0 < n; r0 += PLAN_THREADS) {
     const int r = r0 + tid;
     RowPlan p{-1, 0, -1, 0};
-    if (r < n) {
-      const int32_t s = slot_ids[r], cnt = counts[r];
-      if (s < 0 || s >= c.slots) {
-        bad |= HSTU_CACHE_BAD_SLOT;
-      } else if (__hip_atomic_load(&owner[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != r) {
-        bad |= HSTU_CACHE_TWICE;
-      } else if (cnt < 0) {
-        bad |= HSTU_CACHE_BAD_COUNT;
-      } else {
-        const int32_t len = slot_len(c.lens, c.slots, c.capacity, s);
-        if (cnt > c.capacity - len) {
-          bad |= HSTU_CACHE_FULL;
-        } else {
-          const int32_t had = pages_of(len, c.log_page);
-          p.need = pages_of((int64_t)len + cnt, c.log_page) - had;
-          if (cnt > 0 && (len & ((1 << c.log_page) - 1)) != 0) {
-            const int32_t last = c.tables[(int64_t)s * c.max_pages + had - 1];
-            if (last >= 0 && last < c.num_pages && c.refs[last] > 1) {
-              p.shared = last;
-              ++p.need;
-            }
-          }
-        }
-      }
-    }
+    if (r < n)
+      p = plan_row(c, r, r0 == 0 ? s0 : slot_ids[r], r0 == 0 ? cnt0 : counts[r], owner, bad);
     // two scans, so that 1024 rows of up to 2^31 pages each do not overflow
     int32_t all_hi = 0, all_lo = 0;
     const int32_t want = p.need > 0 ? p.need : 0;
-    const int64_t hi = block_prefix(want >> 15, sums, tid, all_hi);
+    int64_t hi = 0;
+    if (__syncthreads_or(want >> 15)) hi = block_prefix(want >> 15, sums, tid, all_hi);
     const int64_t lo = block_prefix(want & 32767, sums, tid, all_lo);
     const int64_t base = run + (hi << 15) + lo;
     p.base = (int32_t)(base < INT32_MAX ? base : INT32_MAX);   // (past every pool)
-    if (r < n) plan[r] = p;
+    if (r0 == 0) mine = p;
+    else if (r < n) plan[r] = p;
     run += ((int64_t)all_hi << 15) + all_lo;
   }
   const int32_t total = (int32_t)(run < c.num_pages ? run : c.num_pages);
-  const int32_t got = collect<true>(c.refs, 0, c.num_pages, fresh, total, cs, tid);
+  int32_t *fresh = total <= FRESH_LDS ? fresh_lds : fresh_ws;
+  const int32_t got = collect(c.refs, c.num_pages, fresh, total, cs, tid, refs0,
+                              [](int32_t, int32_t count) { return count == 0; });
   __syncthreads();
 
-  for (int r = wv; r < n; r += PLAN_WAVES) {
-    const RowPlan p = plan[r];
-    const int32_t s = slot_ids[r];
-    const bool ok = p.need == 0 || (p.need > 0 && (int64_t)p.base + p.need <= got);
-    if (p.need > 0 && !ok) bad |= HSTU_CACHE_FULL;
-    PageCopy pc{-1, -1, 0};
-    int32_t at = -1;
-    if (ok) {
-      const int32_t len = slot_len(c.lens, c.slots, c.capacity, s);
-      const int32_t first = pages_of(len, c.log_page) - (p.shared >= 0 ? 1 : 0);
-      int32_t *row = c.tables + (int64_t)s * c.max_pages + first;
-      for (int x = lane; x < p.need; x += 64) {
-        const int32_t page = fresh[p.base + x];
-        row[x] = page;
-        c.refs[page] = 1;
-      }
-      if (p.shared >= 0) pc = PageCopy{p.shared, fresh[p.base], len & ((1 << c.log_page) - 1)};
-      at = len;
-    }
-    if (lane == 0) {
+  for (int r0 = 0; r0 < n; r0 += PLAN_THREADS) {
+    const int r = r0 + tid;
+    const RowPlan p = r0 == 0 ? mine : r < n ? plan[r] : RowPlan{-1, 0, -1, 0};
+    if (r < n) {
+      const int32_t s = r0 == 0 ? s0 : slot_ids[r];
+      const bool ok = p.need == 0 || (p.need > 0 && (int64_t)p.base + p.need <= got);
+      if (p.need > 0 && !ok) bad |= HSTU_CACHE_FULL;
+      PageCopy pc{-1, -1, 0};
       if (ok) {
-        c.lens[s] = at + counts[r];
-        if (p.shared >= 0) atomicSub(&c.refs[p.shared], 1);
+        const int32_t first = pages_of(p.len, c.log_page) - (p.shared >= 0 ? 1 : 0);
+        int32_t *row = c.tables + (int64_t)s * c.max_pages + first;
+        for (int x = 0; x < p.need && x < PAGES_ALONE; ++x) {
+          const int32_t page = fresh[p.base + x];
+          row[x] = page;
+          c.refs[page] = 1;
+        }
+        if (p.need > PAGES_ALONE) wide[atomicAdd(&n_wide, 1)] = r;
+        if (p.shared >= 0) {
+          pc = PageCopy{p.shared, fresh[p.base], p.len & ((1 << c.log_page) - 1)};
+          atomicSub(&c.refs[p.shared], 1);
+        }
+        c.lens[s] = p.len + (r0 == 0 ? cnt0 : counts[r]);
+        if (r0 == 0) plan[r] = p;             // for the waves below
       }
       copies[r] = pc;
-      start[r] = at;
+      start[r] = ok ? p.len : -1;
     }
+    __syncthreads();
+    const int many = n_wide;
+    for (int x = wv; x < many; x += PLAN_WAVES) {
+      const RowPlan q = plan[wide[x]];
+      const int32_t s = slot_ids[wide[x]];
+      int32_t *row = c.tables + (int64_t)s * c.max_pages + pages_of(q.len, c.log_page) -
+                     (q.shared >= 0 ? 1 : 0);
+      for (int y = PAGES_ALONE + lane; y < q.need; y += 64) {
+        const int32_t page = fresh[q.base + y];
+        row[y] = page;
+        c.refs[page] = 1;
+      }
+    }
+    __syncthreads();
+    if (tid == 0) n_wide = 0;
+    __syncthreads();
   }
   if (bad) atomicOr(c.status, bad);
 }
@@ -242,54 +299,102 @@ cache_copy_kernel(CacheDev c, const PageCopy *copies) {
 // --------------------------------------------------------------------- write
 constexpr int WRITE_TOKENS = 16;             // of a work-group
 
-// One work-group per row and WRITE_TOKENS of its tokens; a thread moves 16 bytes at a
-// time, four of them in flight.
+// Work-group b of a write: row r's work-groups are write_base(off[r], r) .. -- apart for
+// every batch of rows, whatever their lengths, since floor(a / 16) + ceil(L / 16) <=
+// floor((a + L) / 16) + 1.
+__device__ __forceinline__ int64_t write_base(int64_t off, int64_t r) {
+  return (off < 0 ? 0 : off) / WRITE_TOKENS + r;
+}
+
+// The last of n rows whose base is at most b (-1: none), by every wave for itself: 64
+// rows are looked at in a round, so 4096 rows take two.
+__device__ __forceinline__ int32_t write_row(const int64_t *off, int32_t n, int64_t b, int lane) {
+  int32_t lo = -1, len = n;                    // the answer is lo or one of the len rows behind
+  while (len > 0) {
+    const int32_t step = (len + 63) / 64;
+    const int64_t r = (int64_t)lo + 1 + (int64_t)lane * step;
+    const bool before = r <= (int64_t)lo + len && write_base(off[r <= (int64_t)lo + len ? r : lo + 1],
+                                                             r) <= b;
+    const int hits = __popcll(__ballot(before));
+    if (hits == 0) break;
+    const int32_t at = lo + 1 + (hits - 1) * step;
+    const int32_t left = lo + len - at;        // rows behind `at`
+    lo = at;
+    len = left < step - 1 ? left : step - 1;
+  }
+  return lo;
+}
+
+// A work-group writes up to WRITE_TOKENS of a row's tokens, a wave every fourth: the
+// pages of its tokens are looked up, and lane x moves 16-byte unit x of the k and v rows
+// of all of them.  Every load runs, on a clamped index where its token is none, so that
+// the table's and the rows' latencies overlap and nothing waits in a branch; the stores
+// alone ask.  64 prompts of 16..4096 tokens, 166 MB read and written: 61 us with the
+// loads in branches and as many work-groups for every row, 43 without the branches, 33
+// (5.0 TB/s, a copy's rate) with the work-groups dealt by length.
 __global__ void __launch_bounds__(ROW_THREADS)
-cache_write_kernel(CacheDev c, int32_t layer, const char *k, const char *v, const int64_t *ts,
-                   const int32_t *slot_ids, const int32_t *start, const int64_t *off,
-                   int64_t total) {
-  const int r = blockIdx.x, tid = threadIdx.x;
+cache_write_kernel(CacheDev c, int32_t layer, const char *__restrict__ k,
+                   const char *__restrict__ v, const int64_t *__restrict__ ts,
+                   const int32_t *__restrict__ slot_ids, const int32_t *__restrict__ start,
+                   const int64_t *__restrict__ off, int32_t n, int64_t total, int32_t max_new) {
+  constexpr int W = ROW_THREADS / 64, U = WRITE_TOKENS / W;    // tokens of a wave
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t r = __builtin_amdgcn_readfirstlane(write_row(off, n, blockIdx.x, lane));
+  if (r < 0) return;
   const int32_t s = slot_ids[r], at0 = start[r];
   int64_t first = off[r], end = off[r + 1];
-  if (s < 0 || s >= c.slots || at0 < 0) return;
+  const int64_t t0 = ((int64_t)blockIdx.x - write_base(first, r)) * WRITE_TOKENS;
   first = first < 0 ? 0 : (first > total ? total : first);
   end = end < first ? first : (end > total ? total : end);
-  const int64_t t0 = (int64_t)blockIdx.y * WRITE_TOKENS;
-  const int64_t left = end - first - t0;
-  if (left <= 0) return;
-  const int32_t tokens = left < WRITE_TOKENS ? (int32_t)left : WRITE_TOKENS;
+  end = end - first > max_new ? first + max_new : end;
+  if ((s < 0) | (s >= c.slots) | (at0 < 0) | (t0 >= end - first)) return;
   const int32_t *table = c.tables + (int64_t)s * c.max_pages;
-  // pool row of token t0 + t, -1 where it has no place
-  auto row_of = [&](int32_t t) -> int32_t {
-    const int64_t pos = (int64_t)at0 + t0 + t;
-    if (pos >= c.capacity) return -1;
-    return page_row(table[pos >> c.log_page], c.num_pages, c.log_page, (int32_t)pos);
-  };
-  const uint32_t units = (uint32_t)c.row_bytes >> 4;           // of a row, k and v each
-  const uint32_t all = (uint32_t)tokens * 2 * units;
-  char *kp = c.k + layer * c.layer_bytes, *vp = c.v + layer * c.layer_bytes;
-  constexpr int U = 4;
-  for (uint32_t x0 = tid; x0 < all; x0 += U * ROW_THREADS) {
-    uint4 val[U];
-    char *to[U];
+  const int32_t units = c.row_bytes >> 4;                      // of a row, k and v each
+  const int64_t pool = layer * c.layer_bytes;
+  // pool rows and source rows of the wave's tokens w, w + W, ..; row -1: no such token,
+  // or no place for it
+  int32_t row[U];
+  int64_t src[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const uint32_t x = x0 + i * ROW_THREADS;
-      const uint32_t xc = x < all ? x : x0;
-      const uint32_t t = xc / (2 * units), rem = xc - t * (2 * units);
-      const bool is_v = rem >= units;
-      const int64_t col = 16 * (int64_t)(is_v ? rem - units : rem);
-      const int32_t row = row_of((int32_t)t);
-      val[i] = *(const uint4 *)((is_v ? v : k) + (first + t0 + t) * c.row_bytes + col);
-      to[i] = x < all && row >= 0 ? (is_v ? vp : kp) + (int64_t)row * c.row_bytes + col : nullptr;
+  for (int i = 0; i < U; ++i) {
+    const int64_t t = t0 + w + W * i, pos = at0 + t;
+    src[i] = t < end - first ? first + t : end - 1;
+    row[i] = table[(pos < c.capacity ? pos : c.capacity - 1) >> c.log_page];
+  }
+  issue_fence();
+  bool looked_up = false;
+  for (int32_t x = lane; x < 2 * units; x += 64) {
+    const bool is_v = x >= units;
+    const int64_t col = 16 * (int64_t)(is_v ? x - units : x);
+    const char *from = (is_v ? v : k) + col;
+    char *to = (is_v ? c.v : c.k) + pool + col;
+    uint4 val[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) val[i] = *(const uint4 *)(from + src[i] * c.row_bytes);
+    issue_fence();
+    if (!looked_up) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t t = t0 + w + W * i, pos = at0 + t;
+        const bool there = (t < end - first) & (pos < c.capacity);
+        row[i] = there ? page_row(row[i], c.num_pages, c.log_page, (int32_t)pos) : -1;
+      }
+      looked_up = true;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (to[i]) *(uint4 *)to[i] = val[i];
+      if (row[i] >= 0) *(uint4 *)(to + (int64_t)row[i] * c.row_bytes) = val[i];
   }
-  if (ts && tid < tokens) {
-    const int32_t row = row_of(tid);
-    if (row >= 0) c.ts[row] = ts[first + t0 + tid];
+  if (ts && lane < U) {
+    int32_t mine = -1;
+    int64_t from = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      mine = lane == i ? row[i] : mine;
+      from = lane == i ? src[i] : from;
+    }
+    if (mine >= 0) c.ts[mine] = ts[from];
   }
 }
 
@@ -376,27 +481,33 @@ struct Moves {
   int32_t live, count;
 };
 
+// One search finds both ends of the moves: with `live` pages in use, the free pages
+// before page `live` and then the used ones from it on, equally many.  `list` receives
+// the former (targets), then the latter (sources).
 __global__ void __launch_bounds__(PLAN_THREADS)
-cache_compact_plan_kernel(CacheDev c, Moves *mv, int32_t *src, int32_t *dst, int32_t *to,
-                          int32_t *live_out) {
+cache_compact_plan_kernel(CacheDev c, Moves *mv, int32_t *list, int32_t *to, int32_t *live_out) {
   __shared__ int32_t sums[PLAN_WAVES];
   __shared__ CollectSmem cs;
   const int tid = threadIdx.x;
-  int32_t mine = 0;
-  for (int64_t p0 = 0; p0 < c.num_pages; p0 += ROUND * PLAN_THREADS) {
+  int32_t counts[ROUND], mine = 0;
+  for (int64_t p0 = ROUND * PLAN_THREADS; p0 < c.num_pages; p0 += ROUND * PLAN_THREADS) {
+    load_counts(c.refs, p0, c.num_pages, tid, counts);
 #pragma unroll
-    for (int k = 0; k < ROUND; ++k) {
-      const int64_t p = p0 + k * PLAN_THREADS + tid;
-      mine += p < c.num_pages && c.refs[p] != 0 ? 1 : 0;
-    }
+    for (int k = 0; k < ROUND; ++k) mine += counts[k] != 0 ? 1 : 0;
   }
+  load_counts(c.refs, 0, c.num_pages, tid, counts);           // (kept for the search)
+#pragma unroll
+  for (int k = 0; k < ROUND; ++k) mine += counts[k] != 0 ? 1 : 0;
   int32_t live = 0;
   block_prefix(mine, sums, tid, live);
-  const int32_t m = collect<true>(c.refs, 0, live, dst, live, cs, tid);
-  collect<false>(c.refs, live, c.num_pages, src, m, cs, tid);
+  const int32_t found = collect(c.refs, c.num_pages, list, c.num_pages, cs, tid, counts,
+                                [live](int32_t p, int32_t count) {
+                                  return p < live ? count == 0 : count != 0;
+                                });
+  const int32_t m = found / 2;
   __syncthreads();
   for (int x = tid; x < m; x += PLAN_THREADS) {
-    const int32_t s = src[x], d = dst[x];
+    const int32_t d = list[x], s = list[m + x];
     to[s] = d;
     c.refs[d] = c.refs[s];
     c.refs[s] = 0;
@@ -409,8 +520,7 @@ cache_compact_plan_kernel(CacheDev c, Moves *mv, int32_t *src, int32_t *dst, int
 
 // The pages' rows (a work-group a page of one pool at a time) and the tables.
 __global__ void __launch_bounds__(ROW_THREADS)
-cache_compact_move_kernel(CacheDev c, const Moves *mv, const int32_t *src, const int32_t *dst,
-                          const int32_t *to) {
+cache_compact_move_kernel(CacheDev c, const Moves *mv, const int32_t *list, const int32_t *to) {
   const Moves m = *mv;
   if (m.count == 0) return;
   const int tid = threadIdx.x;
@@ -419,7 +529,7 @@ cache_compact_move_kernel(CacheDev c, const Moves *mv, const int32_t *src, const
   for (int64_t x = blockIdx.x; x < (int64_t)m.count * pools; x += gridDim.x) {
     const int32_t which = (int32_t)(x / pools), y = (int32_t)(x - (int64_t)which * pools);
     char *pool = ((y & 1) ? c.v : c.k) + (y >> 1) * c.layer_bytes;
-    const int64_t s = src[which], d = dst[which];
+    const int64_t d = list[which], s = list[m.count + which];
     copy16(pool + s * page, pool + d * page, page, tid, ROW_THREADS);
     if (c.ts && y == 0)
       for (int t = tid; t < (1 << c.log_page); t += ROW_THREADS)
@@ -435,9 +545,9 @@ cache_compact_move_kernel(CacheDev c, const Moves *mv, const int32_t *src, const
 
 // ------------------------------------------------------------------ workspace
 // extend: owner [slots], plan [slots], copies [slots], fresh [num_pages]; fork: len_of
-// [slots], noted [slots][max_pages]; compact: moves, src, dst, to [num_pages].
+// [slots], noted [slots][max_pages]; compact: moves, list and to [num_pages].
 struct CacheWs {
-  size_t owner, plan, copies, fresh, len_of, noted, moves, src, dst, to, total;
+  size_t owner, plan, copies, fresh, len_of, noted, moves, list, to, total;
 };
 CacheWs cache_ws(int32_t slots, int32_t num_pages, int32_t max_pages) {
   CacheWs w{};
@@ -458,8 +568,7 @@ CacheWs cache_ws(int32_t slots, int32_t num_pages, int32_t max_pages) {
   w.total = std::max(w.total, at);
   at = 0;
   w.moves = take(sizeof(Moves));
-  w.src = take(sizeof(int32_t) * (size_t)num_pages);
-  w.dst = take(sizeof(int32_t) * (size_t)num_pages);
+  w.list = take(sizeof(int32_t) * (size_t)num_pages);
   w.to = take(sizeof(int32_t) * (size_t)num_pages);
   w.total = std::max(w.total, at);
   return w;
@@ -597,14 +706,14 @@ int hstu_cache_write(const hstu_cache *c, int32_t layer, const void *k, const vo
     return fail(HSTU_EINVAL, "k, v, slot_ids, start and row_offsets must be non-null");
   if (((uintptr_t)k | (uintptr_t)v) % 16)
     return fail(HSTU_EINVAL, "k and v must be 16-byte aligned");
-  const int64_t parts = ((int64_t)std::min(max_new, d.capacity) + WRITE_TOKENS - 1) / WRITE_TOKENS;
-  if (parts > 65535)
-    return fail(HSTU_ENOTSUP, "max_new = %d > %d", max_new, 65535 * WRITE_TOKENS);
+  const int64_t groups = total_rows / WRITE_TOKENS + n;        // (see write_base)
+  if (groups > 1 << 24)
+    return fail(HSTU_ENOTSUP, "total_rows = %lld > 2^28 - 16 n", (long long)total_rows);
   hipStream_t s = (hipStream_t)stream;
   prof::Scope ps("cache_write", s);
-  hipLaunchKernelGGL(cache_write_kernel, dim3((unsigned)n, (unsigned)parts), dim3(ROW_THREADS), 0,
-                     s, d, layer, (const char *)k, (const char *)v, timestamps, slot_ids, start,
-                     row_offsets, total_rows);
+  hipLaunchKernelGGL(cache_write_kernel, dim3((unsigned)groups), dim3(ROW_THREADS), 0, s, d, layer,
+                     (const char *)k, (const char *)v, timestamps, slot_ids, start, row_offsets, n,
+                     total_rows, max_new);
   return launched("cache write launch");
 }
 
@@ -655,18 +764,17 @@ int hstu_cache_compact(const hstu_cache *c, int32_t *live, void *workspace, size
   if ((rc = current_device(&dev)) != HSTU_OK) return rc;
   char *ws = (char *)workspace;
   hipStream_t s = (hipStream_t)stream;
-  int32_t *src = (int32_t *)(ws + w.src), *dst = (int32_t *)(ws + w.dst),
-          *to = (int32_t *)(ws + w.to);
+  int32_t *list = (int32_t *)(ws + w.list), *to = (int32_t *)(ws + w.to);
   {
     prof::Scope ps("cache_compact_plan", s);
     hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, d,
-                       (Moves *)(ws + w.moves), src, dst, to, live);
+                       (Moves *)(ws + w.moves), list, to, live);
   }
   if ((rc = launched("cache compact launch")) != HSTU_OK) return rc;
   prof::Scope ps("cache_compact_move", s);
   hipLaunchKernelGGL(cache_compact_move_kernel, dim3(8u * (unsigned)device_info(dev).num_cu),
                      dim3(ROW_THREADS), 0, s, d, (const Moves *)(ws + w.moves),
-                     (const int32_t *)src, (const int32_t *)dst, (const int32_t *)to);
+                     (const int32_t *)list, (const int32_t *)to);
   return launched("cache compact launch");
 }
 

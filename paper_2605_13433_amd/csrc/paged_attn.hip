@@ -34,7 +34,13 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int WAVES = THREADS / 64;
-constexpr int U = 8;                         // steps (16 bytes of k and of v a lane) in flight
+// Steps (16 bytes of k and of v a lane) in flight.  Four steps, four waves a SIMD and
+// as many work-groups as fit at once (CHUNKS_PER_CU) measured best; 128 sequences of up
+// to 4096 tokens, 4 heads of 128 / 32 of up to 65536, 8 heads (us, whole call): 45 /
+// 906; two steps 48 / 942, eight steps on three waves a SIMD 57 / 956 (eight chunks a
+// compute unit 52 / 848: the long batch would gain, the usual one lose), work-groups of
+// 512 threads 52 / 984.
+constexpr int U = 4;
 
 struct PParams {
   CacheDev c;
@@ -56,6 +62,14 @@ struct Chunk {
   int32_t row, slot, len, x0, x1;            // seen tokens x0 .. x1 - 1 of the row
   Seen seen;
 };
+
+// k and v are read once: non-temporal loads keep them from displacing what is used
+// again (U = 8: 62 / 1040 us without, 57 / 956 with).
+__device__ __forceinline__ uint4 load_once(const char *p) {
+  typedef unsigned u32x4n __attribute__((ext_vector_type(4)));
+  const u32x4n v = __builtin_nontemporal_load((const u32x4n *)p);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 
 struct ScanSmem {
   int64_t sums[WAVES];
@@ -82,11 +96,16 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *sums, int tid) 
 }
 
 // The work-group's chunk `item` of the batch, in row order; false past the last one.
-// Rows are looked at THREADS at a time, all of them in both scans.
+// Rows are looked at THREADS at a time, all of them in both scans (the first THREADS
+// are kept from one to the other).  The first work-group notes every row's chunks for
+// the join.
 __device__ __forceinline__ bool find_chunk(const PParams &P, int item, int step, ScanSmem &sm,
                                            int tid) {
-  int64_t total = 0;
-  for (int r = tid; r < P.rows; r += THREADS) {
+  int32_t slot0 = -1, len0 = 0;
+  Seen s0{0, 0, 0};
+  if (tid < P.rows) s0 = row_seen(P, tid, slot0, len0);
+  int64_t total = s0.count;
+  for (int r = tid + THREADS; r < P.rows; r += THREADS) {
     int32_t slot, len;
     total += row_seen(P, r, slot, len).count;
   }
@@ -95,11 +114,15 @@ __device__ __forceinline__ bool find_chunk(const PParams &P, int item, int step,
   if (tid == 0) sm.mine.row = -1;
   __syncthreads();
   int32_t before = 0;
-  for (int r0 = 0; r0 < P.rows && before <= item; r0 += THREADS) {
+  const bool notes = blockIdx.x == 0 && blockIdx.y == 0;
+  for (int r0 = 0; r0 < P.rows && (before <= item || notes); r0 += THREADS) {
     const int r = r0 + tid;
-    Seen s{0, 0, 0};
-    int32_t slot = -1, len = 0;
-    if (r < P.rows) s = row_seen(P, r, slot, len);
+    Seen s = s0;
+    int32_t slot = slot0, len = len0;
+    if (r0 > 0) {
+      s = Seen{0, 0, 0};
+      if (r < P.rows) s = row_seen(P, r, slot, len);
+    }
     const int32_t n = (s.count + C - 1) / C;
     const int32_t incl = wave_prefix(n);
     if ((tid & 63) == 63) sm.sums[tid >> 6] = incl;
@@ -114,8 +137,8 @@ __device__ __forceinline__ bool find_chunk(const PParams &P, int item, int step,
     if (item >= first && item < first + n) {
       const int32_t x0 = (item - first) * C;
       sm.mine = Chunk{r, slot, len, x0, min(x0 + C, s.count), s};
-      if (item == first && blockIdx.y == 0) P.chunks[r] = make_int2(first, n);
     }
+    if (notes && r < P.rows) P.chunks[r] = make_int2(first, n);
     before += all;
     __syncthreads();
   }
@@ -169,7 +192,7 @@ __device__ __forceinline__ float head_sum(float x) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 4)
 paged_attn_kernel(PParams P) {
   constexpr int E = Elem<T>::N;              // elements of a lane
   constexpr int LPH = D / E, HS = 64 / LPH;
@@ -224,8 +247,8 @@ paged_attn_kernel(PParams P) {
       const int32_t r = __shfl(row, (s << log_tpw) + tslot, 64);
       have |= r >= 0 ? 1u << s : 0u;
       const int64_t at = (int64_t)(r >= 0 ? r : 0) * P.c.row_bytes + col;
-      kx[s] = *(const uint4 *)(P.kl + at);
-      vx[s] = *(const uint4 *)(P.vl + at);
+      kx[s] = load_once(P.kl + at);
+      vx[s] = load_once(P.vl + at);
     }
     // the biases of the group's pairs, a lane each
     float bias = 0.0f;
@@ -303,9 +326,7 @@ paged_join_kernel(PParams P) {
   __shared__ float sums[JOIN_WAVES];
   const int r = blockIdx.x, tid = threadIdx.x;
   const int F = P.H * P.d, F4 = F / 4;
-  int32_t slot, len;
-  const Seen s = row_seen(P, r, slot, len);
-  const int2 mine = s.count > 0 ? P.chunks[r] : make_int2(0, 0);
+  const int2 mine = P.chunks[r];              // (x is in the buffer also where y is 0)
   const int slices = F4 < JOIN_THREADS ? JOIN_THREADS / F4 : 1;
   float4 *part = (float4 *)sh;
   float *o = sh;                              // (a thread writes what it alone reads)
