@@ -194,10 +194,37 @@ __device__ __forceinline__ const float *pos_lane(const float *pos, int x0) {
 
 
 
+// Index of a time difference in this set's tables: the causal kernels' is the float's
+// exponent field (KTAB entries, most of which no whole number reaches), the windowed
+// ones' starts at the field of 0.875, so that 0 has entry 0, 1, 2 and 3 have entries 1,
+// 5 and 7, and bucket b from 4 on entry b + 5.  A maximum more per element, but 97
+// entries to stage instead of 604 -- a windowed item is short -- and the runs' sums go
+// to counters by entry, which need no bucket at a run's end (layer-sized training step:
+// 518 -> figures at the launch section).
+constexpr int KT = WINDOWED ? 100 : KTAB;
+__device__ __forceinline__ int tab_index(float delta) {
+  if constexpr (!WINDOWED) return time_index(delta);
+  return time_index(__builtin_fmaxf(__builtin_fabsf(delta), 0.875f)) - 507;
+}
+__device__ __forceinline__ int bucket_of_tab(int k, int nb) {
+  if constexpr (!WINDOWED) return bucket_of_index(k, nb);
+  const int b = k >= 9 ? k - 5 : k >= 7 ? 3 : k >= 5 ? 2 : k >= 1 ? 1 : 0;
+  return b < nb - 1 ? b : nb - 1;
+}
+// Entry of a bucket (the windowed dQ items' counters).
+__device__ __forceinline__ int tab_of_bucket(int b) {
+  return b >= 4 ? b + 5 : b == 3 ? 7 : b == 2 ? 5 : b;
+}
+// Counters of a head: a bucket each, or (windowed) a table entry each, the buckets past
+// the table's end behind it.
+inline __host__ __device__ int time_counters(int nb) {
+  return !WINDOWED ? nb : nb + 6 > KT ? nb + 6 : KT;
+}
+
 // Time tables in dynamic LDS, one slot per head (or a single slot restaged
-// per item when all heads do not fit): KTAB entries by float-exponent index,
+// per item when all heads do not fit): KT entries by float-exponent index,
 // then the nb raw buckets for the exact path.
-__device__ __forceinline__ int time_slot_floats(const KParams &P) { return KTAB + P.nb; }
+__device__ __forceinline__ int time_slot_floats(const KParams &P) { return KT + P.nb; }
 
 // Slots of heads h0 .. h0+nh-1, back to back from `dyn`.  Each thread
 // issues the loads of BATCH entries before it stores any, so staging costs a
@@ -211,8 +238,8 @@ __device__ __forceinline__ void stage_time_heads(const KParams &P, float *dyn, i
     for (int hl = 0; hl < nh; ++hl) {
       const float *tab = P.time_w + (int64_t)(h0 + hl) * P.nb;
       float *slot = dyn + hl * per;
-      for (int x = tid; x < KTAB; x += NT) slot[x] = scale * tab[bucket_of_index(x, P.nb)];
-      for (int x = tid; x < P.nb; x += NT) slot[KTAB + x] = scale * tab[x];
+      for (int x = tid; x < KT; x += NT) slot[x] = scale * tab[bucket_of_tab(x, P.nb)];
+      for (int x = tid; x < P.nb; x += NT) slot[KT + x] = scale * tab[x];
     }
     return;
   }
@@ -223,7 +250,7 @@ __device__ __forceinline__ void stage_time_heads(const KParams &P, float *dyn, i
     for (int k = 0; k < BATCH; ++k) {
       const int i = min(i0 + k * NT, total - 1);         // in bounds, used if < total
       const int hl = i / per, x = i - hl * per;
-      const int src = x < KTAB ? bucket_of_index(x, P.nb) : x - KTAB;
+      const int src = x < KT ? bucket_of_tab(x, P.nb) : x - KT;
       v[k] = P.time_w[(int64_t)(h0 + hl) * P.nb + src];
     }
 #pragma unroll
@@ -974,6 +1001,9 @@ attn_fwd_kernel(KParams P) {
       }
     }
     const int kt_end = min(qt_hi, (it.len - 1) / TILE);       // the item's last key tile
+    // WIN: no pop where two items a work-group, which are dealt, are all there are: in
+    // items of a few steps the work-groups' atomics on the one counter meet
+    const bool pops = !WIN || n_items > 2 * (int)gridDim.x;
     const KeyTiles<WIN> keys(P, QT * it.tile, kt_end);
     const int pos_x = TILE - 1 + TILE * (QT - 1 - sub);       // slice entry of offset 0
     // this lane's bias-slice reads (4 consecutive entries of one copy, see
@@ -1039,7 +1069,7 @@ attn_fwd_kernel(KParams P) {
       // atomic's latency allows), older than this step's loads, so that no
       // wait for them also waits for the atomic
       if (!DIRECT && (WIN ? kn == kt_end || (last && keys.first() == kt_end)
-                          : kt == (kt_end > 0 ? kt_end - 1 : 0)) && tid == 0)
+                          : kt == (kt_end > 0 ? kt_end - 1 : 0)) && tid == 0 && pops)
         nxt2 = atomicAdd(P.pop, 1);     // + 2 gridDim.x where it is published
       if (!last) {         // stream the next key tile into the other buffer
         const int k_valid = it.len - kn * TILE;
@@ -1104,17 +1134,17 @@ attn_fwd_kernel(KParams P) {
             for (int q = 0; q < 2; ++q) {
               const float4 t4 = *(const float4 *)(sm.ts32[pb] + kb + 8 * (2 * hh + q));
               const int r = 8 * hh + 4 * q;
-              x[4 * q + 0] = time_score<D, POS>(s[r], x[4 * q + 0], al2e, ktab[time_index(ts_i32 - t4.x)]);
-              x[4 * q + 1] = time_score<D, POS>(s[r + 1], x[4 * q + 1], al2e, ktab[time_index(ts_i32 - t4.y)]);
-              x[4 * q + 2] = time_score<D, POS>(s[r + 2], x[4 * q + 2], al2e, ktab[time_index(ts_i32 - t4.z)]);
-              x[4 * q + 3] = time_score<D, POS>(s[r + 3], x[4 * q + 3], al2e, ktab[time_index(ts_i32 - t4.w)]);
+              x[4 * q + 0] = time_score<D, POS>(s[r], x[4 * q + 0], al2e, ktab[tab_index(ts_i32 - t4.x)]);
+              x[4 * q + 1] = time_score<D, POS>(s[r + 1], x[4 * q + 1], al2e, ktab[tab_index(ts_i32 - t4.y)]);
+              x[4 * q + 2] = time_score<D, POS>(s[r + 2], x[4 * q + 2], al2e, ktab[tab_index(ts_i32 - t4.z)]);
+              x[4 * q + 3] = time_score<D, POS>(s[r + 3], x[4 * q + 3], al2e, ktab[tab_index(ts_i32 - t4.w)]);
             }
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               x[e] = time_score<D, POS>(
                   s[8 * hh + e], x[e], al2e,
-                  ktab[KTAB + time_bucket(ts_i_item - sm.ts64[pb][kb + c_row(8 * hh + e, 0)],
+                  ktab[KT + time_bucket(ts_i_item - sm.ts64[pb][kb + c_row(8 * hh + e, 0)],
                                           P.nb)]);
           }
         }
@@ -1268,14 +1298,23 @@ struct StreamSmem {
 // The pop's raw return is kept until take_next adds the grid size (the
 // first gridDim.x items are static), so that no arithmetic on it sits next
 // to the atomic.
+template <bool WIN>
 __device__ __forceinline__ void pop_next(const KParams &P, int tid, int &nxt) {
-  if (tid == 0) nxt = atomicAdd(P.pop, 1);
+  // (WIN: not where the dealt items are all there are, as in the forward; nxt stays
+  // past the last one)
+  if (tid == 0 && !(WIN && nxt < 0)) nxt = atomicAdd(P.pop, 1);
 }
 
+template <bool WIN>
 __device__ __forceinline__ int take_next(int *slot, int tid, int nxt) {
-  if (tid == 0) *slot = nxt + (int)gridDim.x;
+  if (tid == 0) *slot = WIN && nxt < 0 ? 0x7fffffff : nxt + (int)gridDim.x;
   lds_barrier();
   return *slot;
+}
+// The first value of a kernel's `nxt`: no pops with WIN where every item is dealt.
+template <bool WIN>
+__device__ __forceinline__ int first_next(int n_items) {
+  return WIN && n_items <= (int)gridDim.x ? -1 : 0;
 }
 
 // A work-list entry carries its sequence's start and length.
@@ -1317,6 +1356,26 @@ __device__ __forceinline__ void dpos_retire_q(typename A::L (*prev)[2 * TILE],
     atomicAdd(&cur[0][x + TILE], v);
   }
 }
+
+// As TimeRun, on counters by table entry (and in natural units: a run's sum takes the
+// factor log2e of the partials where it ends).
+template <typename A>
+struct EntryRun {
+  float sum = 0.0f;
+  int cur = -1;
+  __device__ __forceinline__ void start(int k) { cur = cur < 0 ? k : cur; }
+  __device__ __forceinline__ void add(typename A::L *hist, int cs, int k, float v) {
+    const bool change = k != cur;
+    if (change) atomicAdd(&hist[cur << cs], A::lds(L2E * sum));
+    sum = change ? v : sum + v;
+    cur = k;
+  }
+  __device__ __forceinline__ void flush(typename A::L *hist, int cs) {
+    if (cur >= 0) atomicAdd(&hist[cur << cs], A::lds(L2E * sum));
+    cur = -1;
+    sum = 0.0f;
+  }
+};
 
 // d_time sums of `heads` heads from `h0` on, out of the LDS histogram into one of
 // DTIME_BINS partial tables; the counters are cleared.
@@ -1406,7 +1465,7 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[db][r] = 0.0f;
 
-    TimeRun<A> run;
+    EntryRun<A> run;
     typename A::L *my_t = nullptr;
     typename A::G *dp_item = nullptr;
     if constexpr (TAB && TIME) my_t = tab.hist + h * P.time_hs + (lane & ((1 << P.time_cs) - 1));
@@ -1439,7 +1498,7 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
       const bool slow = TIME && sm.flag[phase & 1] != 0;
       if (TIME && tid == 0) sm.flag[(phase + 1) & 1] = 0;
       if (kt == qt) {
-        pop_next(P, tid, nxt);
+        pop_next<WIN>(P, tid, nxt);
         // K, V registers are free from here: they take the h chunks of the
         // fused silu' store (d=64; at d=128 they are loaded after the loop,
         // which keeps them out of the loop's register peak)
@@ -1498,10 +1557,10 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
               const float4 t4 = *(const float4 *)(sm.ts32 + kb + 8 * (2 * hh + q));
-              tk[4 * q + 0] = time_index(ts_i32 - t4.x);
-              tk[4 * q + 1] = time_index(ts_i32 - t4.y);
-              tk[4 * q + 2] = time_index(ts_i32 - t4.z);
-              tk[4 * q + 3] = time_index(ts_i32 - t4.w);
+              tk[4 * q + 0] = tab_index(ts_i32 - t4.x);
+              tk[4 * q + 1] = tab_index(ts_i32 - t4.y);
+              tk[4 * q + 2] = tab_index(ts_i32 - t4.z);
+              tk[4 * q + 3] = tab_index(ts_i32 - t4.w);
               x[4 * q + 0] += ktab[tk[4 * q + 0]];
               x[4 * q + 1] += ktab[tk[4 * q + 1]];
               x[4 * q + 2] += ktab[tk[4 * q + 2]];
@@ -1511,7 +1570,7 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               tk[e] = time_bucket(ts_i - sm.ts64[kb + c_row(8 * hh + e, 0)], P.nb);
-              x[e] += ktab[KTAB + tk[e]];
+              x[e] += ktab[KT + tk[e]];
             }
           }
         }
@@ -1555,13 +1614,13 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
           if (!slow) {
             if (hh == 0) run.start(tk[0]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) run.add(my_t, P.nb, P.time_cs, tk[e], L2E * dsv[e]);
+            for (int e = 0; e < 8; ++e) run.add(my_t, P.time_cs, tk[e], dsv[e]);
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               float v = L2E * dsv[e];
               asm volatile("" : "+v"(v));       // (as in the dK/dV item)
-              if (v != 0.0f) atomicAdd(&my_t[tk[e] << P.time_cs], A::lds(v));
+              if (v != 0.0f) atomicAdd(&my_t[tab_of_bucket(tk[e]) << P.time_cs], A::lds(v));
             }
           }
         }
@@ -1580,7 +1639,7 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
 
     if (D != 64 && fuse) kr.load(P.h_dq + ooff, q_valid, P.out_stride, tid);
     if constexpr (TAB) {
-      if constexpr (TIME) run.flush(my_t, P.nb, P.time_cs);
+      if constexpr (TIME) run.flush(my_t, P.time_cs);
       lds_barrier();
       if (TIME && P.time_hs == 0) time_fold<DET>(P, tab.hist, tid, h, 1);
       if constexpr (POS) {   // every diagonal of the last window is final
@@ -1668,6 +1727,20 @@ __device__ __forceinline__ void time_fold(const KParams &P, typename TabAcc<DET>
   typedef TabAcc<DET> A;
   typename A::GT *part =
       (typename A::GT *)P.dtime_part + ((int64_t)(blockIdx.x % DTIME_BINS) * P.H + h0) * P.nb;
+  if constexpr (WINDOWED) {          // counters by entry; the entries that no number
+    const int per = time_counters(P.nb);                  // reaches stay 0
+    for (int x = tid; x < heads * per; x += THREADS) {
+      typename A::L v = 0;
+      for (int c = 0; c < 1 << P.time_cs; ++c) {
+        v += tacc[(x << P.time_cs) + c];
+        tacc[(x << P.time_cs) + c] = 0;
+      }
+      const int h = x / per;
+      if (v != 0)
+        atomicAdd(&part[h * P.nb + bucket_of_tab(x - h * per, P.nb)], (typename A::GT)v);
+    }
+    return;
+  }
   for (int x = tid; x < heads * P.nb; x += THREADS) {
     typename A::L v = 0;
     for (int c = 0; c < 1 << P.time_cs; ++c) {
@@ -1821,7 +1894,7 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
       const bool slow = TIME && sm.flag[phase & 1] != 0;
       if (TIME && tid == 0) sm.flag[(phase + 1) & 1] = 0;
       if (qt + 1 == q1) {
-        if constexpr (!FAR) pop_next(P, tid, nxt);
+        if constexpr (!FAR) pop_next<WIN>(P, tid, nxt);
         // Q, dO registers are free from here: they take the h chunks of
         // the fused silu' stores
         if (fuse) {
@@ -1899,10 +1972,10 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
               const float4 t4 = *(const float4 *)(sm.ts32 + ib + 8 * (2 * hh + q));
-              tk[4 * q + 0] = time_index(t4.x - ts_j32);
-              tk[4 * q + 1] = time_index(t4.y - ts_j32);
-              tk[4 * q + 2] = time_index(t4.z - ts_j32);
-              tk[4 * q + 3] = time_index(t4.w - ts_j32);
+              tk[4 * q + 0] = tab_index(t4.x - ts_j32);
+              tk[4 * q + 1] = tab_index(t4.y - ts_j32);
+              tk[4 * q + 2] = tab_index(t4.z - ts_j32);
+              tk[4 * q + 3] = tab_index(t4.w - ts_j32);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] += ktab[tk[e]];
@@ -1910,7 +1983,7 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               tk[e] = time_bucket(sm.ts64[ib + c_row(8 * hh + e, 0)] - ts_j, P.nb);
-              x[e] += ktab[KTAB + tk[e]];
+              x[e] += ktab[KT + tk[e]];
             }
           }
         }
@@ -2142,8 +2215,8 @@ attn_bwd_kernel(KParams P) {
   int phase = 0;
   typename A::G *pend_p = nullptr;
   typename A::G pend_v = 0;
-  int nxt = 0;
-  for (int item = blockIdx.x; item < n_items; item = take_next(&sm.item, tid0, nxt)) {
+  int nxt = first_next<WIN>(n_items);
+  for (int item = blockIdx.x; item < n_items; item = take_next<WIN>(&sm.item, tid0, nxt)) {
     WorkEntry e = P.list[item / P.H];
     const int h = item % P.H;
     if (e.tile & BWD_DQ_FLAG) {
@@ -2181,8 +2254,8 @@ attn_bwd_dq_kernel(KParams P) {
   lds_barrier();
   const TabRefs<DET> tab{smq.mid, smq.low, smq.pwin, hist};
   int phase = 0;
-  int nxt = 0;
-  for (int item = blockIdx.x; item < n_items; item = take_next(&sm.item, tid0, nxt))
+  int nxt = first_next<WIN>(n_items);
+  for (int item = blockIdx.x; item < n_items; item = take_next<WIN>(&sm.item, tid0, nxt))
     dq_item<D, POS, TIME, WIN, DET>(P, sm, tab, dyn, tid0, P.list[item / P.H], item % P.H, phase,
                                     nxt);
   if constexpr (TAB && TIME) {
@@ -2211,8 +2284,8 @@ attn_bwd_dkv_kernel(KParams P) {
   int phase = 0;
   typename A::G *pend_p = nullptr;
   typename A::G pend_v = 0;
-  int nxt = 0;
-  for (int item = blockIdx.x; item < n_items; item = take_next(&sm.item, tid0, nxt))
+  int nxt = first_next<WIN>(n_items);
+  for (int item = blockIdx.x; item < n_items; item = take_next<WIN>(&sm.item, tid0, nxt))
     // K, V stationary in LDS at d=64 (in registers the kernel measured
     // 5-10% slower on the Zipf batch of 1024 sequences)
     dkv_item<D, POS, TIME, DET, D == 64, WIN>(P, smx, dyn, tacc, tid0, P.list[item / P.H],
@@ -2266,7 +2339,7 @@ int persistent_grid(K kernel, size_t dyn, int64_t items, int dev, int block = TH
   return (int)std::max<int64_t>(1, std::min<int64_t>(cap, items));
 }
 
-// Time tables: one slot of KTAB + nb floats per head when all heads fit in
+// Time tables: one slot of KT + nb floats per head when all heads fit in
 // this budget (staged once per work-group), else a single per-item slot.  At
 // d=64 the forward holds half as much: 8 heads of 128 buckets (23 KB) would
 // leave its third work-group no room on a CU (128 power-law sequences 60.6 ->
@@ -2289,16 +2362,18 @@ int64_t dkv128_room(const Problem &p) {
 }
 // a slot of 128 buckets and two counters for each fit
 static_assert(LDS_BYTES / 2 - sizeof(DkvSmem<128, true, false>) >=
-              sizeof(float) * (KTAB + 128) + 2 * sizeof(double) * 128);
+              sizeof(float) * (KT + 128) + 2 * sizeof(double) * 128);
 bool all_heads(const Problem &p, Pass pass) {
   const size_t budget = p.d != 64          ? ALL_HEADS_BUDGET / 4
                         : pass == Pass::FWD ? ALL_HEADS_BUDGET / 2
                                             : ALL_HEADS_BUDGET;
-  if (p.d != 64 && (pass == Pass::DKV || (WINDOWED && pass == Pass::DQ)) && p.H > 1) return false;
-  return p.has_time && sizeof(float) * (size_t)p.H * (KTAB + p.nb) <= budget;
+  if (WINDOWED && p.d != 64 && pass != Pass::FWD)
+    return p.has_time && (int64_t)sizeof(float) * p.H * (KT + p.nb) <= dkv128_room(p) / 2;
+  if (p.d != 64 && pass == Pass::DKV && p.H > 1) return false;
+  return p.has_time && sizeof(float) * (size_t)p.H * (KT + p.nb) <= budget;
 }
 size_t slot_bytes(const Problem &p, bool all) {
-  return p.has_time ? sizeof(float) * (size_t)(all ? p.H : 1) * (KTAB + p.nb) : 0;
+  return p.has_time ? sizeof(float) * (size_t)(all ? p.H : 1) * (KT + p.nb) : 0;
 }
 size_t slots_bytes(const Problem &p, Pass pass) { return slot_bytes(p, all_heads(p, pass)); }
 size_t fwd_dyn_bytes(const Problem &p) { return slots_bytes(p, Pass::FWD); }
@@ -2317,11 +2392,12 @@ TimeHist time_hist(const Problem &p) {
   int64_t room = HIST_BYTES;
   if (p.d != 64)
     room = std::min(room, dkv128_room(p) - (int64_t)slots_bytes(p, Pass::DKV));
-  const bool keep = p.H * (int64_t)p.nb * 8 <= std::min(room, KEEP_BYTES);
+  const int per = time_counters(p.nb);
+  const bool keep = p.H * (int64_t)per * 8 <= std::min(room, KEEP_BYTES);
   TimeHist t;
-  t.n = keep ? p.H * p.nb : p.nb;
+  t.n = keep ? p.H * per : per;
   t.cs = hist_copies_log2(t.n, room);
-  t.hs = keep ? p.nb << t.cs : 0;
+  t.hs = keep ? per << t.cs : 0;
   t.n <<= t.cs;
   return t;
 }
@@ -2418,9 +2494,9 @@ constexpr auto attn_bwd_far = attn_bwd_far_kernel<D, POS, TIME, false>;
 // The forward's items of two query tiles (d = 64 only, see fwd_pairs).
 template <bool X>
 auto attn_fwd_pair_of(const Problem &p) {
-  return p.has_pos ? (p.has_time ? attn_fwd_kernel<64, true, true, 2, false, WINDOWED, X>
-                                 : attn_fwd_kernel<64, true, false, 2, false, WINDOWED, X>)
-                   : (p.has_time ? attn_fwd_kernel<64, false, true, 2, false, WINDOWED, X>
+  return p.has_pos ? (p.has_time ? attn_fwd_kernel<64, true, true, 2, false, WINDOWED, X && WINDOWED>
+                                 : attn_fwd_kernel<64, true, false, 2, false, WINDOWED, X && WINDOWED>)
+                   : (p.has_time ? attn_fwd_kernel<64, false, true, 2, false, WINDOWED, X && WINDOWED>
                                  : attn_fwd_kernel<64, false, false, 2, false, WINDOWED, false>);
 }
 auto attn_fwd_pair(const Problem &p) {
