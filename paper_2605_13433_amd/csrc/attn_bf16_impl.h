@@ -468,30 +468,44 @@ __device__ __forceinline__ void repair_chunk(const KParams &P, int64_t start, in
 
 // What a windowed item's stores need beside the sums: where its rows lie, and the
 // far items' sums of the same rows (far_n tiles of D columns, far_step floats
-// apart, added in order).
-struct RowsOf {
+// apart, added in order); nothing for a causal one.
+template <bool WIN>
+struct RowsOf {};
+template <>
+struct RowsOf<true> {
+  const KParams &P;
   int64_t start;
   int32_t len, h, tile, far_n;
   const float *far;
   int64_t far_step;
 };
-// dK/dV item of key tile e.tile whose own query tiles end before q1.
+template <bool WIN>
+__device__ __forceinline__ RowsOf<WIN> rows_of(const KParams &P, const SeqInfo &si, int h, int tile) {
+  if constexpr (WIN) return RowsOf<WIN>{P, si.start, si.len, h, tile, 0, nullptr, 0};
+  else return RowsOf<WIN>{};
+}
+// dK/dV item of key tile e.tile whose own query tiles end before q1; `part`: 0 dK, 1 dV.
 template <int D, bool WIN>
-__device__ __forceinline__ RowsOf far_rows(const KParams &P, const WorkEntry &e, int h, int q1) {
-  RowsOf ro{e.start, e.len, h, e.tile, 0, nullptr, 0};
+__device__ __forceinline__ RowsOf<WIN> far_rows(const KParams &P, const WorkEntry &e, int h,
+                                                int q1, int part) {
   if constexpr (WIN) {
     const int ntiles = (e.len + TILE - 1) / TILE;
+    RowsOf<WIN> ro{P, e.start, e.len, h, e.tile, 0, nullptr, 0};
     if (P.far_chunk > 0 && e.tile * TILE < P.sinks && q1 < ntiles) {
       const int c0 = q1 / P.far_chunk;
       ro.far_n = (ntiles - 1) / P.far_chunk - c0 + 1;
-      ro.far = far_slot<D>(P, e, h, e.tile, c0);
+      ro.far = far_slot<D>(P, e, h, e.tile, c0) + part * TILE * D;
       ro.far_step = (int64_t)((P.sinks + TILE - 1) / TILE) * P.H * (2 * TILE * D);
     }
+    return ro;
+  } else {
+    return RowsOf<WIN>{};
   }
-  return ro;
 }
 template <int D, Sum M>
-__device__ __forceinline__ void finish_chunk(const KParams &P, const RowsOf &ro, int row, int c8,
+__device__ __forceinline__ void finish_chunk(const RowsOf<false> &, int, int, float (&)[8]) {}
+template <int D, Sum M>
+__device__ __forceinline__ void finish_chunk(const RowsOf<true> &ro, int row, int c8,
                                              float (&f)[8]) {
   for (int c = 0; c < ro.far_n; ++c) {
     const float *p = ro.far + c * ro.far_step + row * D + 8 * c8;
@@ -502,7 +516,7 @@ __device__ __forceinline__ void finish_chunk(const KParams &P, const RowsOf &ro,
   bool odd = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) odd |= !(__builtin_fabsf(f[e]) < __builtin_inff());
-  if (odd) repair_chunk<D, M>(P, ro.start, ro.len, ro.h, ro.tile * TILE + row, c8, f);
+  if (odd) repair_chunk<D, M>(ro.P, ro.start, ro.len, ro.h, ro.tile * TILE + row, c8, f);
 }
 
 // Coalesced bf16 store of a 64 x D fp32 tile in LDS: every thread converts 8
@@ -511,11 +525,11 @@ __device__ __forceinline__ void finish_chunk(const KParams &P, const RowsOf &ro,
 // `silu` set, each value is also multiplied by silu'(h) for the bf16 h of
 // the same chunk in `hv` (a SiLU's backward fused into the store; the
 // caller loads hv early so that its latency is hidden).
-template <int D, bool WIN, Sum M>
-__device__ __forceinline__ void store_rows(const KParams &P, const RowsOf &ro, const float *red,
-                                           int tid, u16 *__restrict__ out,
+template <int D, Sum M, bool WIN>
+__device__ __forceinline__ void store_rows(const float *red, int tid, u16 *__restrict__ out,
                                            int row_stride, int valid, float scale, bool silu,
-                                           const uint4 (&hv)[TILE_CHUNKS<D>]) {
+                                           const uint4 (&hv)[TILE_CHUNKS<D>],
+                                           const RowsOf<WIN> &ro) {
 #pragma unroll
   for (int x = 0; x < TILE_CHUNKS<D>; ++x) {
     const int ch = tid + THREADS * x;
@@ -524,7 +538,7 @@ __device__ __forceinline__ void store_rows(const KParams &P, const RowsOf &ro, c
       const float4 a = *(const float4 *)(red + row * D + 8 * c8);
       const float4 b = *(const float4 *)(red + row * D + 8 * c8 + 4);
       float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      if constexpr (WIN) finish_chunk<D, M>(P, ro, row, c8, f);
+      finish_chunk<D, M>(ro, row, c8, f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] *= scale;
       if (silu) {
@@ -554,9 +568,13 @@ __device__ __forceinline__ void store_rows(const KParams &P, const RowsOf &ro, c
 // atomics are far slower here even without conflicts.)
 // With SUM false the writer waves' blocks are the whole result (no partner
 // adds).
-template <int D, bool SUM = true>
-__device__ __forceinline__ void sum_tile(float *red, const f32x16 (&acc)[D / 32], bool writer,
-                                         int half, int g, int l32) {
+template <int D, Sum M, bool SUM = true, bool WIN>
+__device__ __forceinline__ void sum_store_tile(float *red, const f32x16 (&acc)[D / 32],
+                                               bool writer, int half, int g, int l32,
+                                               int tid, u16 *__restrict__ out,
+                                               int row_stride, int valid, float scale,
+                                               bool silu, const uint4 (&hv)[TILE_CHUNKS<D>],
+                                               const RowsOf<WIN> &ro) {
   lds_barrier();
   if (writer) {
 #pragma unroll
@@ -574,23 +592,33 @@ __device__ __forceinline__ void sum_tile(float *red, const f32x16 (&acc)[D / 32]
         red[(32 * half + c_row(r, g)) * D + 32 * db + l32] += acc[db][r];
   }
   if (SUM) lds_barrier();
+  store_rows<D, M>(red, tid, out, row_stride, valid, scale, silu, hv, ro);
 }
-template <int D, bool WIN, Sum M, bool SUM = true>
-__device__ __forceinline__ void sum_store_tile(const KParams &P, const RowsOf &ro, float *red,
-                                               const f32x16 (&acc)[D / 32],
-                                               bool writer, int half, int g, int l32,
-                                               int tid, u16 *__restrict__ out,
-                                               int row_stride, int valid, float scale,
-                                               bool silu, const uint4 (&hv)[TILE_CHUNKS<D>]) {
-  sum_tile<D, SUM>(red, acc, writer, half, g, l32);
-  store_rows<D, WIN, M>(P, ro, red, tid, out, row_stride, valid, scale, silu, hv);
-}
-// A far item's sum: the tile as it is, in float32.
+// A far item's sum: the tile as it is, in float32.  (The summing is written out in both:
+// as a function of its own it changed the order in which the compiler simplified the
+// causal kernels, whose combined d=64 backward then kept scalars in vector registers, 378
+// more reads of them, and took 3% longer on 128 sequences of up to 512 tokens.)
 template <int D, bool SUM = true>
 __device__ __forceinline__ void sum_keep_tile(float *red, const f32x16 (&acc)[D / 32],
                                               bool writer, int half, int g, int l32, int tid,
                                               float *__restrict__ out) {
-  sum_tile<D, SUM>(red, acc, writer, half, g, l32);
+  lds_barrier();
+  if (writer) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        red[(32 * half + c_row(r, g)) * D + 32 * db + l32] = acc[db][r];
+  }
+  lds_barrier();
+  if (SUM && !writer) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        red[(32 * half + c_row(r, g)) * D + 32 * db + l32] += acc[db][r];
+  }
+  if (SUM) lds_barrier();
 #pragma unroll
   for (int x = 0; x < TILE * D / 4 / THREADS; ++x)
     ((float4 *)out)[tid + THREADS * x] = ((const float4 *)red)[tid + THREADS * x];
@@ -599,18 +627,18 @@ __device__ __forceinline__ void sum_keep_tile(float *red, const f32x16 (&acc)[D 
 // Store of a 64 x D fp32 output tile whose 32 x 32 blocks are held by one
 // wave each: wave (half, cb) holds rows 32*half + c_row(r, g), columns
 // 32*cb + l32 (D = 64: the four waves cover the tile).
-template <int D, bool WIN, Sum M>
-__device__ __forceinline__ void quad_store_tile(const KParams &P, const RowsOf &ro, float *red,
-                                                const f32x16 &acc, int half, int cb,
+template <int D, Sum M, bool WIN>
+__device__ __forceinline__ void quad_store_tile(float *red, const f32x16 &acc, int half, int cb,
                                                 int g, int l32, int tid, u16 *__restrict__ out,
                                                 int row_stride, int valid, float scale,
-                                                bool silu, const uint4 (&hv)[TILE_CHUNKS<D>]) {
+                                                bool silu, const uint4 (&hv)[TILE_CHUNKS<D>],
+                                                const RowsOf<WIN> &ro) {
   static_assert(D == 64, "four 32 x 32 blocks");
   lds_barrier();
 #pragma unroll
   for (int r = 0; r < 16; ++r) red[(32 * half + c_row(r, g)) * D + 32 * cb + l32] = acc[r];
   lds_barrier();
-  store_rows<D, WIN, M>(P, ro, red, tid, out, row_stride, valid, scale, silu, hv);
+  store_rows<D, M>(red, tid, out, row_stride, valid, scale, silu, hv, ro);
 }
 
 // ------------------------------------------------- swizzled DMA-fed tiles
@@ -842,7 +870,8 @@ __device__ __forceinline__ void fwd_item_start(const KParams &P, const Item &it,
 // two key halves: `writer` stores, its partner adds) and its coalesced bf16
 // store by all NT threads; rows at or beyond `valid` are not written.
 template <int D, int NT, bool WIN, bool EXACT>
-__device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, float *red, const f32x16 (&acc)[D / 32], bool mine,
+__device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf<WIN> &ro, float *red,
+                                            const f32x16 (&acc)[D / 32], bool mine,
                                             bool writer, int half, int g, int l32, int tid,
                                             u16 *__restrict__ out, int row_stride, int valid) {
   lds_barrier();
@@ -871,7 +900,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf &ro, 
       const float4 a = *(const float4 *)(red + row * D + 8 * c8);
       const float4 b = *(const float4 *)(red + row * D + 8 * c8 + 4);
       float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      if constexpr (WIN) finish_chunk<D, Sum::O>(P, ro, row, c8, f);
+      finish_chunk<D, Sum::O>(ro, row, c8, f);
       if constexpr (EXACT) {
         float *full = P.o_full + (out - P.out0) + (int64_t)row * row_stride + 8 * c8;
         *(float4 *)full = make_float4(f[0], f[1], f[2], f[3]);
@@ -1197,10 +1226,11 @@ attn_fwd_kernel(KParams P) {
 #pragma unroll
     for (int sq = 0; sq < QT; ++sq) {
       const int tq = QT * it.tile + sq;
-      const RowsOf ro{it.start, it.len, h, tq, 0, nullptr, 0};
-      fwd_store_o<D, NT, WIN, EXACT>(P, ro, (float *)sm.tile[(phase - 1) & 1], oacc, sub == sq, wj == 0, wi, g,
-                         l32, tid, P.out0 + ((it.start + (int64_t)tq * TILE) * P.H + h) * D,
-                         row_stride, it.len - tq * TILE);
+      const RowsOf<WIN> ro = rows_of<WIN>(P, SeqInfo{it.start, it.len, 0}, h, tq);
+      fwd_store_o<D, NT, WIN, EXACT>(P, ro, (float *)sm.tile[(phase - 1) & 1], oacc, sub == sq,
+                                     wj == 0, wi, g, l32, tid,
+                                     P.out0 + ((it.start + (int64_t)tq * TILE) * P.H + h) * D,
+                                     row_stride, it.len - tq * TILE);
     }
     if (!has_next) break;
     cur = nxt;
@@ -1648,10 +1678,9 @@ __device__ __forceinline__ void dq_item(const KParams &P, StreamSmem<D> &sm,
                            dp_item, P.H);
       }
     }
-    const RowsOf ro{si.start, si.len, h, qt, 0, nullptr, 0};
-    sum_store_tile<D, WIN, Sum::DQ>(P, ro, &sm.red[0][0], acc, wj == 0, wi, g, l32, tid,
-                                    P.dq_out + ooff, P.out_stride, q_valid, P.dqk_scale, fuse,
-                                    kr.c);
+    sum_store_tile<D, Sum::DQ>(&sm.red[0][0], acc, wj == 0, wi, g, l32, tid, P.dq_out + ooff,
+                               P.out_stride, q_valid, P.dqk_scale, fuse, kr.c,
+                               rows_of<WIN>(P, si, h, qt));
 }
 
 // ------------------------------------------------------------------ dK/dV
@@ -2129,29 +2158,27 @@ __device__ __forceinline__ void dkv_item(const KParams &P, DkvSmem<D, POS, DET> 
       }
       return;
     }
-    const RowsOf ro = far_rows<D, WIN>(P, e, h, q1);
-    RowsOf ro_v = ro;
-    ro_v.far = ro.far + TILE * D;
     if constexpr (KV_LDS) {
-      if (with_dq) {
-        const RowsOf rq{si.start, si.len, h, 0, 0, nullptr, 0};
-        quad_store_tile<D, WIN, Sum::DQ>(P, rq, &sm.red[0][0],
-                                         dq0_block<D>(dsb, smx.kst, wi, wj, g, lane), wi, wj, g,
-                                         l32, tid, P.dq_out + ooff, P.out_stride, k_valid,
-                                         P.dk_scale_l2, fuse, hq.c);
-      }
+      if (with_dq)
+        quad_store_tile<D, Sum::DQ>(&sm.red[0][0], dq0_block<D>(dsb, smx.kst, wi, wj, g, lane), wi,
+                                    wj, g, l32, tid, P.dq_out + ooff, P.out_stride, k_valid,
+                                    P.dk_scale_l2, fuse, hq.c, rows_of<WIN>(P, si, h, 0));
     }
-    if constexpr (SPLIT)
-      sum_store_tile<D, WIN, Sum::DK, false>(P, ro, &sm.red[0][0], dv, wi == 1, wj, g, l32, tid,
-                                             P.out0 + ooff, P.out_stride, k_valid, P.dk_scale_l2,
-                                             fuse, qr.c);
-    else
-      sum_store_tile<D, WIN, Sum::DK>(P, ro, &sm.red[0][0], dk, wi == 0, wj, g, l32, tid,
-                                      P.out0 + ooff, P.out_stride, k_valid, P.dk_scale_l2, fuse,
-                                      qr.c);
-    sum_store_tile<D, WIN, Sum::DV, !SPLIT>(P, ro_v, &sm.red[0][0], dv, wi == 0, wj, g, l32, tid,
-                                            P.out1 + ooff, P.out_stride, k_valid, P.dv_scale_l2,
-                                            fuse, dr.c);
+    if constexpr (SPLIT) {
+      sum_store_tile<D, Sum::DK, false>(&sm.red[0][0], dv, wi == 1, wj, g, l32, tid, P.out0 + ooff,
+                                        P.out_stride, k_valid, P.dk_scale_l2, fuse, qr.c,
+                                        far_rows<D, WIN>(P, e, h, q1, 0));
+      sum_store_tile<D, Sum::DV, false>(&sm.red[0][0], dv, wi == 0, wj, g, l32, tid, P.out1 + ooff,
+                                        P.out_stride, k_valid, P.dv_scale_l2, fuse, dr.c,
+                                        far_rows<D, WIN>(P, e, h, q1, 1));
+    } else {
+      sum_store_tile<D, Sum::DK>(&sm.red[0][0], dk, wi == 0, wj, g, l32, tid, P.out0 + ooff,
+                                 P.out_stride, k_valid, P.dk_scale_l2, fuse, qr.c,
+                                 far_rows<D, WIN>(P, e, h, q1, 0));
+      sum_store_tile<D, Sum::DV>(&sm.red[0][0], dv, wi == 0, wj, g, l32, tid, P.out1 + ooff,
+                                 P.out_stride, k_valid, P.dv_scale_l2, fuse, dr.c,
+                                 far_rows<D, WIN>(P, e, h, q1, 1));
+    }
 }
 
 // Work-group start of the kernels that run dK/dV items: zeroed d_time
@@ -2222,8 +2249,9 @@ attn_bwd_kernel(KParams P) {
     if (e.tile & BWD_DQ_FLAG) {
       e.tile &= ~BWD_DQ_FLAG;
       // (dO's parts lie where a dK/dV item holds V and its operands)
-      TabRefs<DET> tab{smx.vst, (u16 *)smx.xbuf, nullptr, tacc};
-      if constexpr (POS) tab.pwin = smx.pwin;
+      TabRefs<DET> tab{};
+      if constexpr (WIN) tab = TabRefs<DET>{smx.vst, (u16 *)smx.xbuf, nullptr, tacc};
+      if constexpr (WIN && POS) tab.pwin = smx.pwin;
       dq_item<D, POS, TIME, WIN, DET>(P, sm, tab, dyn, tid0, e, h, phase, nxt);
     } else {
       dkv_item<D, POS, TIME, DET, D == 64, WIN>(P, smx, dyn, tacc, tid0, e, h, phase, pend_p,

@@ -431,7 +431,7 @@ __device__ __forceinline__ void f32_fwd_item(const F32Params &P, F32FwdSmem<D, N
                                rv = rows_of(P, P.v, e, h, D);
   const Run<WIN> run = Run<WIN>::keys(P, i0);
   F32Tile<D> t;
-  t.load(P, rk, FT * run.tile(w), lane);
+  t.load(P, rk, WIN ? FT * run.tile(w) : FT * w, lane);
   float qreg[D / 2];
   load_rows<D>(P, rq, i, g, qreg);
   const F32Bias bias = bias_of(P, e, h, i);
@@ -439,8 +439,9 @@ __device__ __forceinline__ void f32_fwd_item(const F32Params &P, F32FwdSmem<D, N
   clear<D>(acc);
   float *out = P.o + ((e.start + i0) * P.H + h) * D;
 
-  for (int x = w; x < run.count; x += NW) {
-    const int j0 = FT * run.tile(x);
+  const int last = WIN ? run.count - 1 : i0 / FT;
+  for (int x = w; x <= last; x += NW) {
+    const int j0 = FT * (WIN ? run.tile(x) : x);
     t.store(ks, lane);
     stage_ts(P, e, j0, sm.ts[w], lane);
     wave_lds_fence();
@@ -448,10 +449,10 @@ __device__ __forceinline__ void f32_fwd_item(const F32Params &P, F32FwdSmem<D, N
     f32x16 s = tile_scores<D>(ks, qreg, l32, g);
     t.store(vs, lane);
     wave_lds_fence();
-    t.load(P, rk, FT * run.tile(x + NW), lane);
+    t.load(P, rk, WIN ? FT * run.tile(x + NW) : j0 + FT * NW, lane);
     Buckets bk;
     add_bias(P, bias, s, j0 - i, 1, sm.ts[w], g, bk);
-    const bool edge = x == run.count - 1 || win_edge<WIN>(P, i0, j0);
+    const bool edge = x == last || win_edge<WIN>(P, i0, j0);
     float a[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) a[r] = s[r] * sigmoid_f(s[r]) * P.inv_n;
@@ -463,7 +464,7 @@ __device__ __forceinline__ void f32_fwd_item(const F32Params &P, F32FwdSmem<D, N
     }
     tile_accumulate<D>(vs, a, edge, ok, l32, g, acc);
     wave_lds_fence();
-    if (second_round<NW>(x, run.count)) {
+    if (second_round<NW>(x, last + 1)) {
       sum_store<D, NW>(&sm.tile[0][0][0], 2 * FT * F32_ROW<D>, acc, tid, out, P.H * D, e.len - i0,
                        1.0f);
       clear<D>(acc);
@@ -471,7 +472,7 @@ __device__ __forceinline__ void f32_fwd_item(const F32Params &P, F32FwdSmem<D, N
     }
   }
   sum_store<D, NW>(&sm.tile[0][0][0], 2 * FT * F32_ROW<D>, acc, tid, out, P.H * D, e.len - i0,
-                   1.0f, run.count > NW);
+                   1.0f, last >= NW);
 }
 
 template <int D, int NW, bool WIN>
@@ -522,7 +523,7 @@ __device__ __forceinline__ void f32_dq_item(const F32Params &P, F32BwdSmem<D, DE
   const __amdgpu_buffer_rsrc_t rk = rows_of(P, P.k, e, h, D), rv = rows_of(P, P.v, e, h, D);
   const Run<WIN> run = Run<WIN>::keys(P, i0);
   F32Tile<D> t;
-  t.load(P, rk, FT * run.tile(w), lane);
+  t.load(P, rk, WIN ? FT * run.tile(w) : FT * w, lane);
   float qreg[D / 2], oreg[D / 2];
   load_rows<D>(P, rows_of(P, P.q, e, h, D), i, g, qreg);
   load_rows<D>(P, rows_of(P, P.dO, e, h, D), i, g, oreg);
@@ -531,8 +532,9 @@ __device__ __forceinline__ void f32_dq_item(const F32Params &P, F32BwdSmem<D, DE
   clear<D>(acc);
   float *out = P.dq + ((e.start + i0) * P.H + h) * D;
 
-  for (int x = w; x < run.count; x += NW) {
-    const int j0 = FT * run.tile(x);
+  const int last = WIN ? run.count - 1 : i0 / FT;
+  for (int x = w; x <= last; x += NW) {
+    const int j0 = FT * (WIN ? run.tile(x) : x);
     t.store(ks, lane);
     stage_ts(P, e, j0, sm.ts[w], lane);
     wave_lds_fence();
@@ -540,11 +542,11 @@ __device__ __forceinline__ void f32_dq_item(const F32Params &P, F32BwdSmem<D, DE
     f32x16 s = tile_scores<D>(ks, qreg, l32, g);
     t.store(vs, lane);
     wave_lds_fence();
-    t.load(P, rk, FT * run.tile(x + NW), lane);
+    t.load(P, rk, WIN ? FT * run.tile(x + NW) : j0 + FT * NW, lane);
     const f32x16 da = tile_scores<D>(vs, oreg, l32, g);
     Buckets bk;
     add_bias(P, bias, s, j0 - i, 1, sm.ts[w], g, bk);
-    const bool edge = x == run.count - 1 || win_edge<WIN>(P, i0, j0);
+    const bool edge = x == last || win_edge<WIN>(P, i0, j0);
     float ds[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -559,7 +561,7 @@ __device__ __forceinline__ void f32_dq_item(const F32Params &P, F32BwdSmem<D, DE
     }
     tile_accumulate<D>(ks, ds, edge, ok, l32, g, acc);
     wave_lds_fence();
-    if (second_round<NW>(x, run.count)) {
+    if (second_round<NW>(x, last + 1)) {
       sum_store<D, NW>(&sm.tile[0][0][0], 2 * FT * F32_ROW<D>, acc, tid, out, P.H * D, e.len - i0,
                        1.0f);
       clear<D>(acc);
@@ -567,7 +569,7 @@ __device__ __forceinline__ void f32_dq_item(const F32Params &P, F32BwdSmem<D, DE
     }
   }
   sum_store<D, NW>(&sm.tile[0][0][0], 2 * FT * F32_ROW<D>, acc, tid, out, P.H * D, e.len - i0,
-                   P.alpha, run.count > NW);
+                   P.alpha, last >= NW);
 }
 
 template <int D, bool DET, int NW, bool WIN>
@@ -580,8 +582,9 @@ __device__ __forceinline__ void f32_dkv_item(const F32Params &P, F32BwdSmem<D, D
   const int tid = opaque_tid(), lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = j0 + l32;
-  const Run<WIN> qs_run = Run<WIN>::queries(P, j0, e.len);
-  const int first = qs_run.lo, end = first + qs_run.count, tiles = (e.len + FT - 1) / FT;
+  const int first = j0 / FT, tiles = (e.len + FT - 1) / FT;
+  int end = tiles;
+  if constexpr (WIN) end = first + Run<WIN>::queries(P, j0, e.len).count;
   float *qs = sm.tile[w][0], *os = sm.tile[w][1];
   const __amdgpu_buffer_rsrc_t rq = rows_of(P, P.q, e, h, D), ro = rows_of(P, P.dO, e, h, D);
   F32Tile<D> t;
