@@ -46,11 +46,20 @@ HSTU_HD int32_t page_row(int32_t page, int32_t num_pages, int32_t log_page, int3
 }
 
 // Chunk length, in tokens: `total` tokens cut into about `target` chunks, a multiple
-// of `step`.
+// of `step` (where it passes 31 bits, which takes many rows of one long sequence, every
+// row is one chunk).
 HSTU_HD int32_t chunk_len(int64_t total, int32_t target, int32_t step) {
   const int64_t c = (total + target - 1) / target;
   const int64_t r = (c + step - 1) / step * step;
-  return (int32_t)(r < step ? step : r);
+  return (int32_t)(r < step ? step : r > INT32_MAX ? INT32_MAX : r);
+}
+// Chunks of `count` tokens; the end of the chunk that begins at x0.  Neither passes 31
+// bits for any lengths.
+HSTU_HD int32_t chunks_of(int32_t count, int32_t len) {
+  return count > 0 ? (count - 1) / len + 1 : 0;
+}
+HSTU_HD int32_t chunk_end(int32_t x0, int32_t count, int32_t len) {
+  return len < count - x0 ? x0 + len : count;
 }
 
 // Pages that hold `tokens` tokens.

@@ -123,7 +123,7 @@ __device__ __forceinline__ bool find_chunk(const PParams &P, int item, int step,
       s = Seen{0, 0, 0};
       if (r < P.rows) s = row_seen(P, r, slot, len);
     }
-    const int32_t n = (s.count + C - 1) / C;
+    const int32_t n = chunks_of(s.count, C);
     const int32_t incl = wave_prefix(n);
     if ((tid & 63) == 63) sm.sums[tid >> 6] = incl;
     __syncthreads();
@@ -136,7 +136,7 @@ __device__ __forceinline__ bool find_chunk(const PParams &P, int item, int step,
     }
     if (item >= first && item < first + n) {
       const int32_t x0 = (item - first) * C;
-      sm.mine = Chunk{r, slot, len, x0, min(x0 + C, s.count), s};
+      sm.mine = Chunk{r, slot, len, x0, chunk_end(x0, s.count, C), s};
     }
     if (notes && r < P.rows) P.chunks[r] = make_int2(first, n);
     before += all;

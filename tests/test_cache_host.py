@@ -27,6 +27,8 @@ int seen_list(int len, int window, int sinks, int *out, int most) {
 int len_of(const int *lens, int slots, int cap, int slot) { return slot_len(lens, slots, cap, slot); }
 int row_of(int page, int pages, int lp, int pos) { return page_row(page, pages, lp, pos); }
 int chunk(long long total, int target, int step) { return chunk_len(total, target, step); }
+int chunks(int count, int len) { return chunks_of(count, len); }
+int chunk_stop(int x0, int count, int len) { return chunk_end(x0, count, len); }
 int blocks(long long tokens, int lp) { return pages_of(tokens, lp); }
 }
 """
@@ -84,6 +86,20 @@ def test_chunks_fit_the_grid(idx, seed):
     assert int(np.sum(-(-lens // C))) <= target + rows
     # the longest batch that the calls allow
     assert 0 < idx.chunk(65536 * 131072, 1024, 256) < 2 ** 31
+
+
+@pytest.mark.parametrize("rows,count,target", [
+    (65536, 2 ** 31 - 1, 1), (65536, 2 ** 31 - 1, 1024), (65536, 1 << 24, 16), (65536, 1 << 22, 128),
+    (3, 2 ** 31 - 1, 1024), (2, 2 ** 30 + 1, 1), (1, 2 ** 31 - 1, 1), (1, 1, 1024), (65536, 1, 1)])
+def test_chunks_of_the_longest_rows(idx, rows, count, target):
+    """Many rows may name one long sequence: the chunks still fit the grid, follow each
+    other and end with the row."""
+    C = idx.chunk(rows * count, target, 256)
+    n = idx.chunks(count, C)
+    assert C > 0 and n == -(-count // C) and n * rows <= target + rows
+    for x in {0, n // 2, n - 1}:
+        assert idx.chunk_stop(x * C, count, C) == min((x + 1) * C, count)
+    assert idx.chunks(0, C) == 0
 
 
 def test_blocks(idx):
