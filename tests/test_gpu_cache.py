@@ -171,6 +171,39 @@ def test_many_rows_and_pages():
     assert torch.equal(c.v[0][p[x // P], x % P], -rows)
 
 
+@pytest.mark.parametrize("n,most", [(1, 1), (63, 40), (64, 1), (65, 17), (700, 33), (4500, 5)])
+def test_rows_of_every_length(n, most):
+    """Batches of one to thousands of rows, of no tokens up to several work-groups' worth,
+    in any order of the slots; the second call starts inside pages."""
+    rng = np.random.default_rng(n)
+    P = 4
+    b = Both(n * (2 * most // P + 2), P, 1, 32, n + 9000, 2 * most // P + 2, 2, torch.float32,
+             seed=n)
+    for _ in range(2):                  # (more slots than the plan keeps in LDS)
+        b.extend_write(rng.permutation(n + 9000)[:n] if n < 700 else np.arange(n)[::-1].copy(),
+                       rng.integers(0, most + 1, n))
+    b.same()
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 15, 16, 17, 31, 99])
+def test_write_stops_at_max_new(max_new):
+    b = Both(40, 8, 2, 64, 4, 10)
+    counts = np.array([33, 0, 50, 3])
+    slots = np.array([2, 0, 3, 1])
+    start = b.c.extend(i32(slots), i32(counts))
+    want = b.m.extend(slots, counts)
+    off = np.concatenate([[0], np.cumsum(counts)])
+    k, v = (torch.randn(int(off[-1]), 2, 64, generator=b.g).bfloat16() for _ in range(2))
+    ts = torch.arange(int(off[-1])) + 5
+    b.c.write(0, k.cuda(), v.cuda(), i32(slots), start, torch.tensor(off, device="cuda"), max_new,
+              ts.cuda())
+    for r in range(4):                               # the model, a row's first tokens alone
+        n = min(int(counts[r]), max_new)
+        b.m.write(0, k.float().numpy()[off[r]:], v.float().numpy()[off[r]:], slots[r:r + 1],
+                  want[r:r + 1], np.array([0, n]), ts.numpy()[off[r]:])
+    b.same()
+
+
 def test_write_checks_tables_and_offsets_on_the_device():
     """Entries that name no page, starts past the table and offsets past the rows write
     nothing outside; the row behind the last one stays as it was."""

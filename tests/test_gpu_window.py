@@ -269,3 +269,43 @@ def test_two_streams_and_a_graph():
         for a, b in zip(outs(f, g), want):
             assert torch.equal(a, b)
         p0.forward(q, k, v, u, off)
+
+
+@pytest.mark.parametrize("window,sinks", [(40, 0), (0, 3), (64, 70)])
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128),
+                                     (torch.float32, 32)])
+def test_batches_without_tokens(dtype, d, window, sinks):
+    for lens in ([], [0], [0, 0, 0]):
+        w = inputs.make_workload(lens, H=2, d=d, N=100, dtype=dtype, seed=71)
+        got = run(w, window, sinks)
+        assert got["dq"].shape[0] == 0 and got["y"].shape[0] == 0
+        for n in ("d_pos", "d_time"):
+            assert torch.count_nonzero(got[n]) == 0, n
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128),
+                                     (torch.float32, 64)])
+def test_checked_offsets(monkeypatch, dtype, d):
+    """HSTU_VALIDATE=1: valid offsets give what an unchecked call gives, others are
+    reported and no pair is worked on."""
+    w = inputs.make_workload([300, 0, 1, 129], H=2, d=d, N=300, dtype=dtype, seed=73)
+    plain = run(w, 70, 5, det=True)
+    monkeypatch.setenv("HSTU_VALIDATE", "1")
+    q, k, v, u, off = (to_dev(x) for x in (w.q, w.k, w.v, w.u, w.seq_offsets))
+    plan = hstu.Plan(q, off, w.N, to_dev(w.pos_w), to_dev(w.time_w), to_dev(w.timestamps),
+                     w.num_buckets, backward=True, deterministic=True, window=70, sinks=5)
+    f = plan.forward(q, k, v, u, off)
+    assert plan.status() == 0
+    g = plan.backward(q, k, v, u, off, to_dev(w.dy))
+    assert plan.status(backward=True) == 0
+    for n, t in (("y", f.y), ("dq", g.dq), ("dk", g.dk), ("dv", g.dv), ("d_pos", g.d_pos_w),
+                 ("d_time", g.d_time_w)):
+        check(n, wide(t), wide(plain[n]), TOL[torch.float32] if n.startswith("d_") else TOL[dtype])
+    bad = off.clone()
+    bad[1], bad[2] = 310, 300                              # too long, then decreasing
+    bits = hstu.HSTU_SEQ_TOO_LONG | hstu.HSTU_SEQ_DECREASING
+    plan.forward(q, k, v, u, bad)
+    assert plan.status() == bits
+    g = plan.backward(q, k, v, u, bad, to_dev(w.dy))
+    assert plan.status(backward=True) == bits
+    assert torch.isfinite(g.d_pos_w).all() and torch.isfinite(g.d_time_w).all()
