@@ -420,51 +420,72 @@ __device__ __forceinline__ float *far_slot(const KParams &P, const WorkEntry &e,
 // A pair that is not seen has the weight 0, but the products multiply it all
 // the same, and 0 times an infinity or a NaN of the other row's would be a NaN in a
 // row that must not see it.  Such a row shows in its sum, which then is not
-// finite: the thread that stores eight values of it adds them up again over the
-// pairs that are seen alone, from memory, on the vector ALU.  This costs a test of
-// the stored values (one in 16 or more that an item adds up) instead of a look at
-// every tile's rows.
+// finite: the thread that stored eight values of it adds them up again over the
+// pairs that are seen alone, from memory, on the vector ALU, and stores them once more.
+// This costs a test of the stored values (one in 16 or more that an item adds up)
+// instead of a look at every tile's rows.
+//
 enum class Sum { O, DQ, DK, DV };
-template <int D, Sum M>
-__device__ __forceinline__ void repair_chunk(const KParams &P, int64_t start, int len, int h,
-                                             int x, int c8, float (&f)[8]) {
-  constexpr bool ROWS = M == Sum::O || M == Sum::DQ;      // x is a query, y its keys
-  constexpr bool BACK = M == Sum::DQ || M == Sum::DK;     // weighted by dS, not by A
+// Chunks c of the output tile's 16-byte chunks (8 columns) with bit x of `odd` set,
+// c = tid + nt * x.
+template <int D>
+__device__ __forceinline__ void repair_chunks(const KParams &P, Sum M, int64_t start, int len,
+                                              int h, int tile, int tid, int nt, uint32_t odd) {
+  const bool rows = M == Sum::O || M == Sum::DQ;          // x is a query, y its keys
+  const bool back = M == Sum::DQ || M == Sum::DK;         // weighted by dS, not by A
   const int64_t step = (int64_t)P.H * D, head = start * step + (int64_t)h * D;
-  const u16 *own = (ROWS ? P.q : P.k) + head + x * step;
-  const u16 *own_d = (ROWS ? P.dO : P.v) + head + x * step;
-  const int recent = x - P.window + 1 > 0 ? x - P.window + 1 : 0;
-  const int first = ROWS ? (min(P.sinks, recent) > 0 ? 0 : recent) : x;
-  const int end = ROWS ? x + 1 : (x < P.sinks || P.window > len - x ? len : x + P.window);
+#pragma unroll 1
+  for (int bit = 0; odd >> bit; ++bit) {
+    if (!((odd >> bit) & 1)) continue;
+    const int ch = tid + nt * bit;
+    const int x = tile * TILE + ch / (D / 8), c8 = ch % (D / 8);
+    const u16 *own = (rows ? P.q : P.k) + head + x * step;
+    const u16 *own_d = (rows ? P.dO : P.v) + head + x * step;
+    const int recent = x - P.window + 1 > 0 ? x - P.window + 1 : 0;
+    const int head_end = min(P.sinks, recent);            // (rows)
+    const int first = rows ? (head_end > 0 ? 0 : recent) : x;
+    const int end = rows ? x + 1 : (x < P.sinks || P.window > len - x ? len : x + P.window);
+    float f[8] = {};
+#pragma unroll 1
+    for (int y = first; y < end; y = rows && y + 1 == head_end ? recent : y + 1) {
+      const u16 *oth = (rows ? P.k : P.q) + head + y * step;
+      const u16 *oth_d = (rows ? P.v : P.dO) + head + y * step;
+      float s = 0.0f, da = 0.0f;
+#pragma unroll 1
+      for (int c = 0; c < D; ++c) {
+        s = __builtin_fmaf(bf2f(own[c]), bf2f(oth[c]), s);
+        if (back) da = __builtin_fmaf(bf2f(own_d[c]), bf2f(oth_d[c]), da);
+      }
+      const int i = rows ? x : y, j = rows ? y : x;
+      s *= P.alpha;
+      if (P.pos_w) s += P.pos_w[(int64_t)h * (2 * P.N - 1) + (j - i + P.N - 1)];
+      if (P.time_w)
+        s += P.time_w[h * P.nb + time_bucket(P.ts[start + i] - P.ts[start + j], P.nb)];
+      const float sg = sigmoid_f(s);
+      const float w = back ? da * sg * __builtin_fmaf(s, 1.0f - sg, 1.0f) : s * sg;
+      const u16 *add = (M == Sum::O    ? P.v
+                        : M == Sum::DQ ? P.k
+                        : M == Sum::DK ? P.q
+                                       : P.dO) + head + y * step + 8 * c8;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = 0.0f;
-#pragma unroll 1
-  for (int y = first; y < end; y = ROWS && y + 1 == min(P.sinks, recent) ? recent : y + 1) {
-    const u16 *oth = (ROWS ? P.k : P.q) + head + y * step;
-    const u16 *oth_d = (ROWS ? P.v : P.dO) + head + y * step;
-    float s = 0.0f, da = 0.0f;
-#pragma unroll 1
-    for (int c = 0; c < D; ++c) {
-      s = __builtin_fmaf(bf2f(own[c]), bf2f(oth[c]), s);
-      if (BACK) da = __builtin_fmaf(bf2f(own_d[c]), bf2f(oth_d[c]), da);
+      for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(w, bf2f(add[e]), f[e]);
     }
-    const int i = ROWS ? x : y, j = ROWS ? y : x;
-    s *= P.alpha;
-    if (P.pos_w) s += P.pos_w[(int64_t)h * (2 * P.N - 1) + (j - i + P.N - 1)];
-    if (P.time_w)
-      s += P.time_w[h * P.nb + time_bucket(P.ts[start + i] - P.ts[start + j], P.nb)];
-    const float sg = sigmoid_f(s);
-    // in the units of the kernel's own sum (see dq_ds, dkv_ds)
-    const float w = M == Sum::O    ? s * sg / (float)P.N
-                    : M == Sum::DV ? L2E * s * sg
-                                   : (M == Sum::DK ? L2E : 1.0f) * da * sg *
-                                         __builtin_fmaf(s, 1.0f - sg, 1.0f);
-    const u16 *add = (M == Sum::O    ? P.v
-                      : M == Sum::DQ ? P.k
-                      : M == Sum::DK ? P.q
-                                     : P.dO) + head + y * step + 8 * c8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(w, bf2f(add[e]), f[e]);
+    const int64_t at = (start + x) * P.out_stride + h * D + 8 * c8;
+    const u16 *silu = M == Sum::O    ? nullptr
+                      : M == Sum::DQ ? P.h_dq
+                      : M == Sum::DK ? P.h_dk
+                                     : P.h_dv;
+    u16 *out = (M == Sum::DQ ? P.dq_out : M == Sum::DV ? P.out1 : P.out0) + at;
+    // (one value at a time: few registers)
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      float g = f[0] * (back ? P.dqk_scale : P.inv_n);
+      f[0] = f[1], f[1] = f[2], f[2] = f[3], f[3] = f[4];
+      f[4] = f[5], f[5] = f[6], f[6] = f[7];
+      if (M == Sum::O && P.o_full) P.o_full[at + e] = g;
+      if (silu) g *= dsilu_f(bf2f(silu[at + e]));
+      out[e] = (u16)(pack2(g, g) & 0xffffu);
+    }
   }
 }
 
@@ -482,7 +503,8 @@ struct RowsOf<true> {
   int64_t far_step;
 };
 template <bool WIN>
-__device__ __forceinline__ RowsOf<WIN> rows_of(const KParams &P, const SeqInfo &si, int h, int tile) {
+__device__ __forceinline__ RowsOf<WIN> rows_of(const KParams &P, const SeqInfo &si, int h,
+                                               int tile) {
   if constexpr (WIN) return RowsOf<WIN>{P, si.start, si.len, h, tile, 0, nullptr, 0};
   else return RowsOf<WIN>{};
 }
@@ -504,10 +526,9 @@ __device__ __forceinline__ RowsOf<WIN> far_rows(const KParams &P, const WorkEntr
     return RowsOf<WIN>{};
   }
 }
-template <int D, Sum M>
-__device__ __forceinline__ void finish_chunk(const RowsOf<false> &, int, int, float (&)[8]) {}
-template <int D, Sum M>
-__device__ __forceinline__ void finish_chunk(const RowsOf<true> &ro, int row, int c8,
+// Adds the far sums; returns whether a value is not finite.
+template <int D>
+__device__ __forceinline__ bool finish_chunk(const RowsOf<true> &ro, int row, int c8,
                                              float (&f)[8]) {
   for (int c = 0; c < ro.far_n; ++c) {
     const float *p = ro.far + c * ro.far_step + row * D + 8 * c8;
@@ -518,7 +539,31 @@ __device__ __forceinline__ void finish_chunk(const RowsOf<true> &ro, int row, in
   bool odd = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) odd |= !(__builtin_fabsf(f[e]) < __builtin_inff());
-  if (odd) repair_chunk<D, M>(ro.P, ro.start, ro.len, ro.h, ro.tile * TILE + row, c8, f);
+  return odd;
+}
+// The d=128 backward calls it: inlined, at its two or three stores, it took registers from
+// the loops (training step of 32 sequences of up to 4096 tokens, 4 heads of 128: 488 us
+// called, 502 inlined, 518 inlined at every eight values; 488 without any).  The call's
+// own registers would cost the d=64 backward without tables one of three waves a SIMD,
+// and the forward kernels scratch memory (the eight-wave one so much that the runtime
+// gives it out anew at every launch, a millisecond), so these inline it.  A call cannot
+// be handed the kernel's arguments by reference without their being copied to scratch
+// memory: it reads them from where the launch put them (the kernels' one argument is a
+// KParams).
+template <int D>
+__device__ __attribute__((noinline, cold)) void repair_call(const KParams *args, Sum M,
+                                                            int64_t start, int len, int h,
+                                                            int tile, int tid, uint32_t odd) {
+  repair_chunks<D>(*args, M, start, len, h, tile, tid, THREADS, odd);
+}
+template <int D, Sum M>
+__device__ __forceinline__ void repair(const RowsOf<true> &ro, int tid, int nt, uint32_t odd) {
+  if (__builtin_expect(odd == 0, true)) return;
+  if constexpr (M == Sum::O || D == 64)
+    repair_chunks<D>(ro.P, M, ro.start, ro.len, ro.h, ro.tile, tid, nt, odd);
+  else
+    repair_call<D>((const KParams *)__builtin_amdgcn_kernarg_segment_ptr(), M, ro.start, ro.len,
+                   ro.h, ro.tile, tid, odd);
 }
 
 // Coalesced bf16 store of a 64 x D fp32 tile in LDS: every thread converts 8
@@ -532,6 +577,7 @@ __device__ __forceinline__ void store_rows(const float *red, int tid, u16 *__res
                                            int row_stride, int valid, float scale, bool silu,
                                            const uint4 (&hv)[TILE_CHUNKS<D>],
                                            const RowsOf<WIN> &ro) {
+  uint32_t odd = 0;
 #pragma unroll
   for (int x = 0; x < TILE_CHUNKS<D>; ++x) {
     const int ch = tid + THREADS * x;
@@ -540,7 +586,7 @@ __device__ __forceinline__ void store_rows(const float *red, int tid, u16 *__res
       const float4 a = *(const float4 *)(red + row * D + 8 * c8);
       const float4 b = *(const float4 *)(red + row * D + 8 * c8 + 4);
       float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      finish_chunk<D, M>(ro, row, c8, f);
+      if constexpr (WIN) odd |= finish_chunk<D>(ro, row, c8, f) ? 1u << x : 0u;
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] *= scale;
       if (silu) {
@@ -559,6 +605,7 @@ __device__ __forceinline__ void store_rows(const float *red, int tid, u16 *__res
       *(uint4 *)(out + (int64_t)row * row_stride + 8 * c8) = pk;
     }
   }
+  if constexpr (WIN) repair<D, M>(ro, tid, THREADS, odd);
 }
 
 // Cross-wave sum of a 64 x D fp32 output tile and its coalesced bf16 store.
@@ -894,6 +941,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf<WIN> 
   }
   lds_barrier();
   constexpr int CH = TILE * D / 8 / NT;
+  uint32_t odd = 0;
 #pragma unroll
   for (int x = 0; x < CH; ++x) {
     const int ch = tid + NT * x;
@@ -902,7 +950,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf<WIN> 
       const float4 a = *(const float4 *)(red + row * D + 8 * c8);
       const float4 b = *(const float4 *)(red + row * D + 8 * c8 + 4);
       float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      finish_chunk<D, Sum::O>(ro, row, c8, f);
+      if constexpr (WIN) odd |= finish_chunk<D>(ro, row, c8, f) ? 1u << x : 0u;
       if constexpr (EXACT) {
         float *full = P.o_full + (out - P.out0) + (int64_t)row * row_stride + 8 * c8;
         *(float4 *)full = make_float4(f[0], f[1], f[2], f[3]);
@@ -916,6 +964,7 @@ __device__ __forceinline__ void fwd_store_o(const KParams &P, const RowsOf<WIN> 
       *(uint4 *)(out + (int64_t)row * row_stride + 8 * c8) = pk;
     }
   }
+  if constexpr (WIN) repair<D, Sum::O>(ro, tid, NT, odd);
 }
 
 // ---------------------------------------------------------------- forward

@@ -200,6 +200,25 @@ def test_unseen_rows_leave_no_trace(dtype, d, bad):
         check(n, got[n][~touched], clean[n][~touched], TOL[dtype])
 
 
+@pytest.mark.parametrize("pos,time", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("L", [50, 64, 300])
+@pytest.mark.parametrize("d", [64, 128])
+def test_unseen_rows_of_the_first_tile(d, L, pos, time):
+    """As above for a row of the first tile, with and without tables (which sum dQ of
+    those rows in different places); the rows before it must not see it."""
+    w = inputs.make_workload([L, 3, L], H=2, d=d, N=L, pos=pos, time=time, seed=62)
+    row, window, sinks = 40, 30, 2
+    clean = {n: wide(t) for n, t in run(w, window, sinks).items() if t is not None}
+    w.k[L + 3 + row, 0, 1] = float("nan")
+    w.v[L + 3 + row, 1, 1] = float("inf")
+    got = {n: wide(t) for n, t in run(w, window, sinks).items() if t is not None}
+    m = ref.seen(L, window, sinks)
+    hit = np.zeros(2 * L + 3, bool)
+    hit[L + 3:] = m[:, row]
+    for n in ("o", "y", "dq", "du"):
+        check(n, got[n][~hit], clean[n][~hit], TOL[torch.bfloat16])
+
+
 def test_differences():
     """The gradients in fp32 along random directions against central differences of
     the forward in float64 (the definition)."""
