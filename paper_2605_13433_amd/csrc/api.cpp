@@ -350,8 +350,8 @@ int attn_bwd_call(const void *q, const void *k, const void *v, const void *u,
   if (p.T > 0) {
     // the LayerNorm backward launch also builds the work lists
     prof::Scope ps("ln_bwd", s);
-    e = launch_ln_bwd_sched(p, io->dy, u, io->o, win ? win->o_full : nullptr, io->ln_mean, io->ln_rstd, io->du,
-                            ws + L.dO,
+    e = launch_ln_bwd_sched(p, io->dy, u, io->o, win ? win->o_full : nullptr, io->ln_mean,
+                            io->ln_rstd, io->du, ws + L.dO,
                             (L.dpos_part && p.dtype == HSTU_BF16) ? ws + L.dpos_part : nullptr,
                             seq_offsets, ws, L, go, s);
     if (e != hipSuccess) return hip_fail(e, "layernorm backward launch");

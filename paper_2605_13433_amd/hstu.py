@@ -244,6 +244,9 @@ def make_window(window, sinks=0, o_full=None) -> Optional[Window]:
         if sinks:
             raise ValueError("sinks are given without a window")
         return None
+    for name, x in (("window", window), ("sinks", sinks)):
+        if not 0 <= int(x) < 1 << 31:      # (a C int would take it modulo 2^32)
+            raise ValueError(f"{name} = {x} is not in [0, 2^31)")
     return Window(int(window), int(sinks), _ptr(o_full))
 
 

@@ -72,3 +72,8 @@ def test_python_refusals():
     with pytest.raises(ValueError, match="without a window"):
         hstu.make_window(None, 3)
     assert hstu.make_window(None) is None
+    for window, sinks in ((-1, 0), (1 << 31, 0), ((1 << 32) + 5, 0), (5, -1), (5, 1 << 32)):
+        with pytest.raises(ValueError, match="not in"):
+            hstu.make_window(window, sinks)
+    w = hstu.make_window((1 << 31) - 1, 0)
+    assert (w.window, w.sinks) == ((1 << 31) - 1, 0)
