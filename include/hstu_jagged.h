@@ -217,8 +217,8 @@ size_t hstu_jagged_attn_workspace_bytes(int32_t B, int32_t max_len, int32_t H,
  *
  * Work and memory grow with total_tokens x (window + sinks).  The backward of
  * HSTU_BF16 takes a further workspace, twice q's size with a bias table (dO's further
- * bits), and for the sinks' gradients over the queries past their windows about q's
- * size and 2 x 64 x d x H floats per sequence and 64 sinks.
+ * bits), and, where sequences may be long, for the sinks' gradients over the queries
+ * past their windows about q's size and 2 x 64 x d x H floats per sequence and 64 sinks.
  * ------------------------------------------------------------------------- */
 typedef struct {
     int32_t window;              /* >= 0                                     */

@@ -235,7 +235,18 @@ Layout make_layout(const Problem &p, bool for_bwd, int dev) {
   if (bf16_bwd && p.windowed && p.sinks > 0) {
     const int64_t tiles = ceil_div(p.N, TILE), reach = ((int64_t)TILE - 2 + p.window) / TILE;
     const int64_t sink_tiles = ceil_div(p.sinks, TILE);
-    if (reach < tiles - 1) {
+    // query tiles of a sink tile's chain past its windows, and the steps that every one of
+    // two work-groups a compute unit has (both item kinds)
+    const int64_t chain = tiles - 1 - reach;
+    const int64_t steps = ceil_div(p.T, TILE) * (reach + 1 + sink_tiles) * 2 * p.H /
+                          (2 * (int64_t)L.num_cu);
+    // A pass of its own costs some ten steps, and where the work-groups have many steps
+    // the chain runs beside them.  Backward without and with the pass (us): 128 sequences
+    // of up to 512 tokens, 4 heads of 64, window 128 (chain 5) 83 and 98, 64 of up to 2048,
+    // window 256 (chain 27) 118 and 132, 128 of up to 4096, window 256 (59) 827 and 869;
+    // one of 2048, window 64 (30) 63 and 40, 8 of up to 4096, window 256 (59) 126 and 89,
+    // 24 of up to 8192, window 512 (119) 412 and 389.
+    if (chain > 10 + std::min(2 * steps, 16 + steps / 4)) {
       L.far_after = (int32_t)reach;
       L.far_chunk = (int32_t)(FAR_CHUNK * sink_tiles);
       L.far_entries = p.T / ((int64_t)TILE * L.far_chunk) + p.B;

@@ -115,8 +115,8 @@ struct Layout {
 
 // Query tiles of a far chunk (times the sink tiles): short enough that the chunks of a
 // few long sequences fill the device (32 of up to 4096 tokens, 4 heads of 128: far pass
-// 52 us with 16, 27 with 4; 128 of up to 512, 4 of 64: 17.7 and 16.6), long enough that a
-// chunk's two float32 tiles stay at half of the rows it reads.
+// 52 us with 16, 27 with 4), long enough that a chunk's two float32 tiles stay at half
+// of the rows it reads.
 constexpr int FAR_CHUNK = 4;
 
 // ---- host helpers shared by the C-ABI translation units ----

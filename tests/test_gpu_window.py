@@ -105,6 +105,22 @@ def test_far_sinks(d, window, sinks):
     against(w, window, sinks)
 
 
+@pytest.mark.parametrize("pos,time", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_far_sinks_and_tables(d, pos, time):
+    w = inputs.make_workload([3000, 70, 1], H=2, d=d, N=3000, pos=pos, time=time, seed=77)
+    against(w, 100, 66)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_far_sinks_among_many_items(d):
+    # long chains in a batch whose backward takes two launches
+    rng = np.random.default_rng(d)
+    lens = [int(x) for x in rng.integers(0, 400, 350)] + [4000, 2500]
+    w = inputs.make_workload(lens, H=2, d=d, N=4000, seed=78)
+    against(w, 60, 70)
+
+
 @pytest.mark.parametrize("d,H,n,window,sinks", [(64, 4, 400, 100, 5), (128, 2, 250, 90, 0),
                                                 (64, 2, 700, 30, 66)])
 def test_many_items(d, H, n, window, sinks):
