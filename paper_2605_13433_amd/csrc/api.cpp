@@ -246,13 +246,18 @@ Layout make_layout(const Problem &p, bool for_bwd, int dev) {
     // window 256 (chain 27) 118 and 132, 128 of up to 4096, window 256 (59) 827 and 869;
     // one of 2048, window 64 (30) 63 and 40, 8 of up to 4096, window 256 (59) 126 and 89,
     // 24 of up to 8192, window 512 (119) 412 and 389.
-    if (chain > 10 + std::min(2 * steps, 16 + steps / 4)) {
+    // The room is there in any case, so that a workspace for some tokens holds for fewer.
+    if (chain > 0) {
       L.far_after = (int32_t)reach;
       L.far_chunk = (int32_t)(FAR_CHUNK * sink_tiles);
       L.far_entries = p.T / ((int64_t)TILE * L.far_chunk) + p.B;
       L.list_f = take(sizeof(WorkEntry) * (size_t)std::max<int64_t>(L.far_entries, 1));
       L.far_part = take(sizeof(float) * 2 * TILE * (size_t)p.d * p.H * (size_t)sink_tiles *
                         (size_t)std::max<int64_t>(L.far_entries, 1));
+      if (chain <= 10 + std::min(2 * steps, 16 + steps / 4)) {
+        L.far_chunk = 0;
+        L.far_entries = 0;
+      }
     }
   }
   L.total = at;

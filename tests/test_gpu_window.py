@@ -344,3 +344,14 @@ def test_checked_offsets(monkeypatch, dtype, d):
     g = plan.backward(q, k, v, u, bad, to_dev(w.dy))
     assert plan.status(backward=True) == bits
     assert torch.isfinite(g.d_pos_w).all() and torch.isfinite(g.d_time_w).all()
+
+
+@pytest.mark.parametrize("bias", [True, False])
+@pytest.mark.parametrize("B,N,window,sinks", [(256, 2048, 64, 4), (40, 4096, 500, 130), (3, 300, 9, 1)])
+def test_a_workspace_holds_for_fewer_tokens(B, N, window, sinks, bias):
+    t = torch.zeros(1, device="cuda")
+    rab = hstu.make_rab(t if bias else None, None, None, 128, 1.0)
+    win = hstu.make_window(window, sinks, t)
+    sizes = [hstu.hstu_jagged_window_attn_workspace_bytes(B, N, 4, 64, T, 1, hstu.HSTU_BF16, rab, win)
+             for T in sorted((1, 100, 1000, 5000, 20000, 60000, B * N // 2, B * N))]
+    assert sizes == sorted(sizes)
