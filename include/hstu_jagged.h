@@ -214,8 +214,8 @@ size_t hstu_jagged_attn_workspace_bytes(int32_t B, int32_t max_len, int32_t H,
  * the plain call).  With a table, the forward therefore also hands o on in float32
  * (o_full, which LayerNorm then reads), and the backward carries dO to 24 bits: the
  * table gradients are as exact as those of HSTU_F32.
- * (dq, dk and dv are rounded to bf16 and read dO in bf16: on sequences of a few
- * tokens, where <dO, v> cancels, dq and dk may be 1e-2 off.)
+ * (dk and dv, and dq without a table, read dO in bf16: on sequences of a few tokens,
+ * where <dO, v> cancels, dq and dk may be 1e-2 off.)
  *
  * Work and memory grow with total_tokens x (window + sinks).  The backward of
  * HSTU_BF16 takes a further workspace, twice q's size with a bias table (dO's further
